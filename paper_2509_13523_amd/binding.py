@@ -31,7 +31,10 @@ EXPORTS = ("aeris_winattn_fwd", "aeris_winattn_bwd", "aeris_winattn_bwd_stages",
            "aeris_gate_residual_bwd_workspace_bytes", "aeris_gate_residual_bwd",
            "aeris_swiglu_fwd", "aeris_swiglu_bwd", "aeris_norm_linear_workspace_bytes",
            "aeris_norm_linear_fwd", "aeris_norm_linear_swiglu_fwd", "aeris_linear_fwd",
-           "aeris_linear_bwd_workspace_bytes", "aeris_linear_bwd")
+           "aeris_linear_bwd_workspace_bytes", "aeris_linear_bwd",
+           # include/aeris_fp8.h
+           "aeris_fp8_scale_pitch", "aeris_fp8_quantize", "aeris_residual_norm_fp8_fwd", "aeris_swiglu_fp8_fwd",
+           "aeris_linear_fp8_fwd", "aeris_linear_fp8_bwd_workspace_bytes", "aeris_linear_fp8_bwd")
 
 
 class aeris_winattn_params(ctypes.Structure):
@@ -155,6 +158,20 @@ def load():
     lib.aeris_linear_bwd_workspace_bytes.restype = sz
     lib.aeris_linear_bwd.argtypes = [vp, vp, vp, i64, i32, i32, vp, vp, vp, sz, vp]
     lib.aeris_linear_bwd.restype = ctypes.c_int
+    lib.aeris_fp8_scale_pitch.argtypes = [i32]
+    lib.aeris_fp8_scale_pitch.restype = i32
+    lib.aeris_fp8_quantize.argtypes = [vp, i32, i64, i32, vp, vp, vp, vp, vp]
+    lib.aeris_fp8_quantize.restype = ctypes.c_int
+    lib.aeris_residual_norm_fp8_fwd.argtypes = [vp, vp, vp, vp, vp, vp, f32, i64, i64, i32, vp, vp, vp, vp, vp]
+    lib.aeris_residual_norm_fp8_fwd.restype = ctypes.c_int
+    lib.aeris_swiglu_fp8_fwd.argtypes = [vp, i64, i32, vp, vp, vp]
+    lib.aeris_swiglu_fp8_fwd.restype = ctypes.c_int
+    lib.aeris_linear_fp8_fwd.argtypes = [vp, vp, vp, vp, i64, i32, i32, vp, vp]
+    lib.aeris_linear_fp8_fwd.restype = ctypes.c_int
+    lib.aeris_linear_fp8_bwd_workspace_bytes.argtypes = [i64, i32, i32]
+    lib.aeris_linear_fp8_bwd_workspace_bytes.restype = sz
+    lib.aeris_linear_fp8_bwd.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, sz, vp]
+    lib.aeris_linear_fp8_bwd.restype = ctypes.c_int
     _lib = lib
     return lib
 
@@ -737,4 +754,131 @@ def aeris_linear_bwd(x, weight, dy, want_dx=True, want_dweight=True, dx=None, dw
                                  workspace.data_ptr(), workspace.numel(), _stream())
     if rc != 0:
         raise AerisError(rc, "aeris_linear_bwd")
+    return (dx if want_dx else None), (dweight if want_dweight else None)
+
+
+# ---------------------------------------------------------------------------------------------
+# include/aeris_fp8.h: the 8-bit path of the projections.  A quantised matrix is a pair of
+# contiguous CUDA tensors: values torch.float8_e4m3fn [rows, cols] and scales torch.float8_e8m0fnu
+# [rows, aeris_fp8_scale_pitch(cols)], one per 128 columns.
+# ---------------------------------------------------------------------------------------------
+def aeris_fp8_scale_pitch(cols):
+    return load().aeris_fp8_scale_pitch(cols)
+
+
+def _empty_quantized(rows, cols, device):
+    import torch
+    return (torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=device),
+            torch.empty((rows, -(-cols // 512) * 4), dtype=torch.float8_e8m0fnu, device=device))
+
+
+def _quantized(q, scales):
+    import torch
+    assert q.is_cuda and q.is_contiguous() and q.dtype == torch.float8_e4m3fn and q.dim() == 2
+    assert scales.is_cuda and scales.is_contiguous() and scales.dtype == torch.float8_e8m0fnu
+    assert scales.shape == (q.shape[0], -(-q.shape[1] // 512) * 4)
+    return q.shape[0], q.shape[1]
+
+
+def aeris_fp8_quantize(x, rows=True, transposed=False):
+    """x [n, C] bf16 or fp32.  Returns (x8, xs, xt8, xts): x quantised by rows and its transpose
+    quantised by rows; entries not asked for are None."""
+    import torch
+    assert x.is_cuda and x.is_contiguous() and x.dim() == 2 and x.dtype in (torch.bfloat16, torch.float32)
+    n, c = x.shape
+    x8, xs = _empty_quantized(n, c, x.device) if rows else (None, None)
+    xt8, xts = _empty_quantized(c, n, x.device) if transposed else (None, None)
+    rc = load().aeris_fp8_quantize(x.data_ptr(), AERIS_DT_F32 if x.dtype == torch.float32 else AERIS_DT_BF16,
+                                   n, c, _ptr(x8), _ptr(xs), _ptr(xt8), _ptr(xts), _stream())
+    if rc != 0:
+        raise AerisError(rc, "aeris_fp8_quantize")
+    return x8, xs, xt8, xts
+
+
+def aeris_residual_norm_fp8_fwd(x, y, alpha, w, gamma, beta, eps, rows_per_sample, s=None, want_r=True):
+    """s = x + alpha_b * y, h = RMSNorm(s; w) * (1 + gamma_b) + beta_b.  Returns (s, r, h8, hs); with y None
+    nothing is added and s is x.  s may be passed in, also as x or y."""
+    import torch
+    n, c = _rows(x)
+    _f32(w, gamma, beta, alpha)
+    if y is None:
+        s = x
+    else:
+        assert _rows(y) == (n, c)
+        if s is None:
+            s = torch.empty_like(x)
+        assert _rows(s) == (n, c)
+    r = torch.empty(n, dtype=torch.float32, device=x.device) if want_r else None
+    h8, hs = _empty_quantized(n, c, x.device)
+    rc = load().aeris_residual_norm_fp8_fwd(x.data_ptr(), _ptr(y), _ptr(alpha), w.data_ptr(), gamma.data_ptr(),
+                                            beta.data_ptr(), float(eps), n, rows_per_sample, c,
+                                            None if y is None else s.data_ptr(), _ptr(r), h8.data_ptr(),
+                                            hs.data_ptr(), _stream())
+    if rc != 0:
+        raise AerisError(rc, "aeris_residual_norm_fp8_fwd")
+    return s, r, h8, hs
+
+
+def aeris_swiglu_fp8_fwd(uv):
+    """(g8, gs): g = silu(u) * v for uv = [u | v], quantised."""
+    n, c2 = _rows(uv)
+    assert c2 % 2 == 0
+    g8, gs = _empty_quantized(n, c2 // 2, uv.device)
+    rc = load().aeris_swiglu_fp8_fwd(uv.data_ptr(), n, c2 // 2, g8.data_ptr(), gs.data_ptr(), _stream())
+    if rc != 0:
+        raise AerisError(rc, "aeris_swiglu_fp8_fwd")
+    return g8, gs
+
+
+def aeris_linear_fp8_fwd(x8, xs, w8, ws, y=None):
+    """y [n, F] bf16 = x w^T of quantised x [n, C] and w [F, C]."""
+    import torch
+    n, c = _quantized(x8, xs)
+    f, cw = _quantized(w8, ws)
+    assert c == cw
+    if y is None:
+        y = torch.empty((n, f), dtype=torch.bfloat16, device=x8.device)
+    assert _rows(y) == (n, f)
+    rc = load().aeris_linear_fp8_fwd(x8.data_ptr(), xs.data_ptr(), w8.data_ptr(), ws.data_ptr(), n, c, f,
+                                     y.data_ptr(), _stream())
+    if rc != 0:
+        raise AerisError(rc, "aeris_linear_fp8_fwd")
+    return y
+
+
+def aeris_linear_fp8_bwd_workspace_bytes(n_rows, channels, out_features):
+    return load().aeris_linear_fp8_bwd_workspace_bytes(n_rows, channels, out_features)
+
+
+def aeris_linear_fp8_bwd(x8, xs, wt8, wts, dy, want_dx=True, want_dweight=True, dx=None, dweight=None,
+                         workspace=None):
+    """Gradients of y = x w^T: dx = Q(dy) w (bf16) from the quantised transposed weight wt8 [C, F],
+    dweight = dy^T x (fp32).  x8, xs may be None without want_dweight, wt8, wts without want_dx."""
+    import torch
+    n, f = _rows(dy)
+    if want_dx:
+        c, fw = _quantized(wt8, wts)
+        assert fw == f
+    if want_dweight:
+        nx, cx = _quantized(x8, xs)
+        assert nx == n and (not want_dx or cx == c)
+        c = cx
+    if not (want_dx or want_dweight):
+        raise ValueError("aeris_linear_fp8_bwd: neither dx nor dweight is wanted")
+    if want_dx and dx is None:
+        dx = torch.empty((n, c), dtype=torch.bfloat16, device=dy.device)
+    if want_dweight and dweight is None:
+        dweight = torch.empty((f, c), dtype=torch.float32, device=dy.device)
+    assert not want_dx or _rows(dx) == (n, c)
+    assert not want_dweight or (dweight.shape == (f, c) and dweight.is_contiguous() and dweight.dtype == torch.float32)
+    if workspace is None:
+        workspace = torch.empty(max(aeris_linear_fp8_bwd_workspace_bytes(n, c, f), 16), dtype=torch.uint8,
+                                device=dy.device)
+    rc = load().aeris_linear_fp8_bwd(_ptr(x8) if want_dweight else None, _ptr(xs) if want_dweight else None,
+                                     _ptr(wt8) if want_dx else None, _ptr(wts) if want_dx else None,
+                                     dy.data_ptr(), n, c, f, dx.data_ptr() if want_dx else None,
+                                     dweight.data_ptr() if want_dweight else None, workspace.data_ptr(),
+                                     workspace.numel() * workspace.element_size(), _stream())
+    if rc != 0:
+        raise AerisError(rc, "aeris_linear_fp8_bwd")
     return (dx if want_dx else None), (dweight if want_dweight else None)

@@ -1,0 +1,475 @@
+// Rows that leave in 8 bits (argument contracts in include/aeris_fp8.h): quantised bf16 or fp32 rows and
+// their transpose, gated residual + RMSNorm + modulation, SwiGLU gate, and the way back to bf16.
+//
+// All of them are bound by memory traffic: every input is read once, results leave once, with fp32
+// arithmetic in between.  A block of 128 columns lies in 16 lanes, eight columns each, so its largest
+// magnitude is three instructions per lane pair and four rotations inside a row of lanes, without the LDS.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "aeris_fp8.h"
+#include "aeris_layer_ops.h"
+#include "aeris_winattn.h"
+#include "fp8_common.hpp"
+#include "fp8_rows.hpp"
+#include "winattn_launch.hpp"
+
+namespace aeris {
+namespace {
+
+constexpr int kThreads256 = 256;
+constexpr int kGroups = kThreads256 / kBlockLanes;   // blocks a workgroup works on side by side
+constexpr unsigned kMostBlocks = 8192;               // workgroups of a launch over blocks
+
+// Blocks a workgroup's 16 groups of lanes walk over: all blocks of the rows [r0, r1), 16 apart.
+struct BlockWalk {
+  long long row, end;
+  int block, blocks;
+  int row_step, block_step;
+  __device__ __forceinline__ void init(long long n_rows, int cols) {
+    blocks = (cols + AERIS_FP8_BLOCK - 1) / AERIS_FP8_BLOCK;
+    const int group = threadIdx.x / kBlockLanes;
+    const long long r0 = n_rows * blockIdx.x / gridDim.x;
+    end = n_rows * (blockIdx.x + 1) / gridDim.x;
+    row = r0 + group / blocks;
+    block = group % blocks;
+    row_step = kGroups / blocks;
+    block_step = kGroups % blocks;
+  }
+  __device__ __forceinline__ bool valid() const { return row < end; }
+  __device__ __forceinline__ void step() {
+    row += row_step;
+    block += block_step;
+    if (block >= blocks) {
+      block -= blocks;
+      row += 1;
+    }
+  }
+};
+// Workgroups for such a walk: whole rows each, about four blocks per group of lanes.
+unsigned walk_grid(long long n_rows, int cols) {
+  const long long blocks = (cols + AERIS_FP8_BLOCK - 1) / AERIS_FP8_BLOCK;
+  const long long rows_each = (4 * kGroups + blocks - 1) / blocks;
+  const long long want = (n_rows + rows_each - 1) / rows_each;
+  return (unsigned)(want < (long long)kMostBlocks ? want : (long long)kMostBlocks);
+}
+
+// ---- rows of bf16 or fp32, by rows -----------------------------------------------------------------
+template <typename T>
+__global__ __launch_bounds__(kThreads256) void fp8_quantize_rows_kernel(const T* __restrict__ x, long long n_rows,
+                                                                        int cols, unsigned char* __restrict__ x8,
+                                                                        unsigned char* __restrict__ xs) {
+  const int lane = threadIdx.x & (kBlockLanes - 1), pitch = scale_pitch(cols);
+  BlockWalk at;
+  at.init(n_rows, cols);
+  // every lane of a wave takes part in the rotations, so all leave together
+  for (; __any(at.valid()); at.step()) {
+    const int c = at.block * AERIS_FP8_BLOCK + lane * 8;
+    const bool in = at.valid() && c < cols;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (in) {
+      Raw8<T> raw;
+      raw.load(x + at.row * cols + c);
+      raw.values(v);
+    }
+    u32x2 q;
+    const uint32_t byte = quantize_block(v, q);
+    if (in) *reinterpret_cast<u32x2*>(x8 + at.row * cols + c) = q;
+    if (at.valid()) store_scale(xs + at.row * pitch, at.block, at.blocks, pitch, byte, lane);
+  }
+}
+
+// ---- the transpose, and by rows from the same read ---------------------------------------------------
+// A workgroup takes 128 rows x 128 columns: thread t holds rows 8 (t / 16) ... + 7 of columns
+// 8 (t % 16) ... + 7.  Columns' maxima: over a thread's rows, over the four threads of a wave that share
+// columns, over the waves through the LDS.  The transposed bytes pass through the LDS: row of 128 bytes per
+// column, eight-byte chunks XORed with the column so that neither side meets many bank conflicts.
+template <typename T>
+__global__ __launch_bounds__(kThreads256) void fp8_quantize_transposed_kernel(
+    const T* __restrict__ x, int n_rows, int cols, unsigned char* __restrict__ x8, unsigned char* __restrict__ xs,
+    unsigned char* __restrict__ xt8, unsigned char* __restrict__ xts) {
+  __shared__ __align__(16) uint32_t most_of[kThreads256 / 64][AERIS_FP8_BLOCK];
+  __shared__ __align__(16) unsigned char turned[AERIS_FP8_BLOCK * AERIS_FP8_BLOCK];
+  const int lane = threadIdx.x & 15, strip = threadIdx.x >> 4, wave = threadIdx.x >> 6;
+  const int blocks = (cols + AERIS_FP8_BLOCK - 1) / AERIS_FP8_BLOCK;
+  const int row_blocks = (n_rows + AERIS_FP8_BLOCK - 1) / AERIS_FP8_BLOCK;
+  const int block = blockIdx.x % blocks, row_block = blockIdx.x / blocks;
+  const int c = block * AERIS_FP8_BLOCK + lane * 8, r0 = row_block * AERIS_FP8_BLOCK + strip * 8;
+  const int pitch = scale_pitch(cols), t_pitch = scale_pitch(n_rows);
+  const bool in = c < cols && r0 < n_rows;         // n_rows % 64 == 0: all eight rows or none
+
+  Raw8<T> raw[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+    if (in) raw[i].load(x + (long long)(r0 + i) * cols + c);
+  auto values = [&](int i, float (&v)[8]) __attribute__((always_inline)) {
+    if (in) {
+      raw[i].values(v);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = 0.f;
+    }
+  };
+  if (x8 != nullptr) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float v[8];
+      values(i, v);
+      u32x2 q;
+      const uint32_t byte = quantize_block(v, q);
+      if (in) *reinterpret_cast<u32x2*>(x8 + (long long)(r0 + i) * cols + c) = q;
+      if (r0 < n_rows) store_scale(xs + (long long)(r0 + i) * pitch, block, blocks, pitch, byte, lane);
+    }
+  }
+
+  uint32_t most[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float v[8];
+    values(i, v);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t a = __float_as_uint(v[e]) & 0x7fffffffu;
+      most[e] = a < kNotFinite && a > most[e] ? a : most[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+#pragma unroll
+    for (int d = 16; d < 64; d <<= 1) {
+      const uint32_t o = (uint32_t)__shfl_xor((int)most[e], d, 64);
+      most[e] = most[e] > o ? most[e] : o;
+    }
+  }
+  if ((threadIdx.x & 63) < kBlockLanes) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) most_of[wave][lane * 8 + e] = most[e];
+  }
+  __syncthreads();
+  uint32_t byte[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    uint32_t m = most_of[0][lane * 8 + e];
+#pragma unroll
+    for (int w = 1; w < kThreads256 / 64; ++w) m = m > most_of[w][lane * 8 + e] ? m : most_of[w][lane * 8 + e];
+    byte[e] = scale_byte(m);
+  }
+  uint32_t q[8][2];                                  // [column][rows 0-3, 4-7]
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    float v[4][8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) values(4 * h + i, v[i]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float inverse = scale_inverse(byte[e]);
+      const int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0][e] * inverse, v[1][e] * inverse, 0, false);
+      q[e][h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[2][e] * inverse, v[3][e] * inverse, w, true);
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int col = lane * 8 + e;
+    *reinterpret_cast<u32x2*>(turned + col * 128 + ((strip ^ ((lane << 1) & 15)) << 3)) = u32x2{q[e][0], q[e][1]};
+  }
+  __syncthreads();
+  // 16 bytes per thread and pass: 8 threads per column
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const int col = i * 32 + (threadIdx.x >> 3), piece = threadIdx.x & 7;      // bytes 16 piece ... + 15
+    const int turn = ((col >> 3) << 1) & 15;
+    const u32x4 v = *reinterpret_cast<const u32x4*>(turned + col * 128 + (((2 * piece) ^ turn) << 3));
+    const int gc = block * AERIS_FP8_BLOCK + col, gr = row_block * AERIS_FP8_BLOCK + piece * 16;
+    if (gc < cols && gr < n_rows) *reinterpret_cast<u32x4*>(xt8 + (long long)gc * n_rows + gr) = v;
+  }
+  // the column scales: threads 0 ... 15 hold those of all 128 columns
+  if (threadIdx.x < kBlockLanes && c < cols) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      unsigned char* row = xts + (long long)(c + e) * t_pitch;
+      row[row_block] = (unsigned char)byte[e];
+      if (row_block == row_blocks - 1)
+        for (int b = row_blocks; b < t_pitch; ++b) row[b] = kScaleOne;
+    }
+  }
+}
+
+// ---- back to bf16, exact ---------------------------------------------------------------------------
+__global__ __launch_bounds__(kThreads256) void fp8_dequantize_kernel(const unsigned char* __restrict__ x8,
+                                                                     const unsigned char* __restrict__ xs,
+                                                                     long long n_rows, int cols,
+                                                                     bf16_t* __restrict__ x) {
+  const int lane = threadIdx.x & (kBlockLanes - 1), pitch = scale_pitch(cols);
+  BlockWalk at;
+  at.init(n_rows, cols);
+  for (; at.valid(); at.step()) {
+    const int c = at.block * AERIS_FP8_BLOCK + lane * 8;
+    if (c >= cols) continue;
+    const u32x2 q = *reinterpret_cast<const u32x2*>(x8 + at.row * cols + c);
+    const float scale = __uint_as_float((uint32_t)xs[at.row * pitch + at.block] << 23);
+    u32x4 o;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[h], false);
+      const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)q[h], true);
+      o[2 * h] = pack_bf16(lo[0] * scale, lo[1] * scale);
+      o[2 * h + 1] = pack_bf16(hi[0] * scale, hi[1] * scale);
+    }
+    *reinterpret_cast<u32x4*>(x + at.row * cols + c) = o;
+  }
+}
+
+// ---- gated residual + RMSNorm + modulation --------------------------------------------------------------
+// A wave per row at a time, K vectors of eight channels per lane, a workgroup on a contiguous chunk of the
+// rows of one sample, whose modulation it keeps in the LDS: w (1 + gamma), beta, alpha.  The row stays in
+// registers between its sum of squares and its result.  The expressions are those of
+// aeris_gate_residual_fwd and aeris_rmsnorm_adaln_fwd, so that s and r have their bits.
+constexpr int kRowWaves = 4;
+constexpr int kTargetChunks = 2048;
+
+struct NormParams {
+  const bf16_t* x;
+  const bf16_t* y;          // null: nothing to add
+  const float *alpha, *w, *gamma, *beta;
+  float eps;
+  long long rows_per_sample;
+  int chunks;               // workgroups per sample
+  int C;
+  bf16_t* s;
+  float* r;
+  unsigned char *h8, *hs;
+};
+
+__device__ __forceinline__ void unpack8(const u32x4& raw, float (&f)[8]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f[2 * i] = __uint_as_float(raw[i] << 16);
+    f[2 * i + 1] = __uint_as_float(raw[i] & 0xffff0000u);
+  }
+}
+
+template <int K, bool kResidual>
+__global__ __launch_bounds__(kThreads256) void residual_norm_fp8_kernel(NormParams p) {
+  extern __shared__ __align__(16) float lds_f[];
+  const int C = p.C;
+  float *s_lds = lds_f, *b_lds = lds_f + C, *a_lds = lds_f + 2 * C;
+  const int sample = blockIdx.x / p.chunks, chunk = blockIdx.x - sample * p.chunks;
+  const long long base = sample * p.rows_per_sample;
+  const long long r0 = base + p.rows_per_sample * chunk / p.chunks;
+  const long long r1 = base + p.rows_per_sample * (chunk + 1) / p.chunks;
+  for (int c = threadIdx.x; c < C; c += kThreads256) {
+    s_lds[c] = p.w[c] * (1.f + p.gamma[(long long)sample * C + c]);
+    b_lds[c] = p.beta[(long long)sample * C + c];
+    if (kResidual) a_lds[c] = p.alpha[(long long)sample * C + c];
+  }
+  __syncthreads();
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const float inv_c = 1.f / (float)C;
+  const int blocks = (C + AERIS_FP8_BLOCK - 1) / AERIS_FP8_BLOCK, pitch = scale_pitch(C);
+  for (long long row = r0 + wave; row < r1; row += kRowWaves) {
+    const u32x4* src = reinterpret_cast<const u32x4*>(p.x + row * C);
+    const u32x4* add = kResidual ? reinterpret_cast<const u32x4*>(p.y + row * C) : nullptr;
+    u32x4 raw[K], more[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int v = k * 64 + lane;
+      const bool in = v * 8 < C;
+      raw[k] = in ? __builtin_nontemporal_load(&src[v]) : u32x4{0, 0, 0, 0};
+      if (kResidual) more[k] = in ? __builtin_nontemporal_load(&add[v]) : u32x4{0, 0, 0, 0};
+    }
+    if (kResidual) {
+      u32x4* dst = reinterpret_cast<u32x4*>(p.s + row * C);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const int v = k * 64 + lane;
+        if (v * 8 < C) {
+          float f[8], g[8];
+          unpack8(raw[k], f);
+          unpack8(more[k], g);
+          const f32x4 a0 = *reinterpret_cast<const f32x4*>(a_lds + v * 8);
+          const f32x4 a1 = *reinterpret_cast<const f32x4*>(a_lds + v * 8 + 4);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float lo = __builtin_fmaf((i < 2 ? a0 : a1)[2 * i & 3], g[2 * i], f[2 * i]);
+            const float hi = __builtin_fmaf((i < 2 ? a0 : a1)[(2 * i + 1) & 3], g[2 * i + 1], f[2 * i + 1]);
+            raw[k][i] = pack_bf16(lo, hi);
+          }
+          __builtin_nontemporal_store(raw[k], &dst[v]);
+        }
+      }
+    }
+    float ss = 0.f;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      float f[8];
+      unpack8(raw[k], f);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(f[i], f[i], ss);
+    }
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, 64);
+    const float r = 1.f / __builtin_sqrtf(ss * inv_c + p.eps);
+    if (p.r != nullptr && lane == 0) p.r[row] = r;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const int v = k * 64 + lane;
+      const bool in = v * 8 < C;
+      float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      if (in) {
+        float f[8];
+        unpack8(raw[k], f);
+        const f32x4 s0 = *reinterpret_cast<const f32x4*>(s_lds + v * 8);
+        const f32x4 s1 = *reinterpret_cast<const f32x4*>(s_lds + v * 8 + 4);
+        const f32x4 b0 = *reinterpret_cast<const f32x4*>(b_lds + v * 8);
+        const f32x4 b1 = *reinterpret_cast<const f32x4*>(b_lds + v * 8 + 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          o[i] = __builtin_fmaf(f[i] * r, s0[i], b0[i]);
+          o[4 + i] = __builtin_fmaf(f[4 + i] * r, s1[i], b1[i]);
+        }
+      }
+      u32x2 q;
+      const uint32_t byte = quantize_block(o, q);
+      if (in) __builtin_nontemporal_store(q, reinterpret_cast<u32x2*>(p.h8 + row * C) + v);
+      const int block = v / kBlockLanes;
+      if (block < blocks) store_scale(p.hs + row * pitch, block, blocks, pitch, byte, lane);
+    }
+  }
+}
+
+// ---- SwiGLU gate ------------------------------------------------------------------------------------
+__global__ __launch_bounds__(kThreads256) void swiglu_fp8_kernel(const bf16_t* __restrict__ uv, long long n_rows,
+                                                                 int hidden, unsigned char* __restrict__ g8,
+                                                                 unsigned char* __restrict__ gs) {
+  const int lane = threadIdx.x & (kBlockLanes - 1), pitch = scale_pitch(hidden);
+  BlockWalk at;
+  at.init(n_rows, hidden);
+  for (; __any(at.valid()); at.step()) {
+    const int c = at.block * AERIS_FP8_BLOCK + lane * 8;
+    const bool in = at.valid() && c < hidden;
+    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (in) {
+      const bf16_t* src = uv + at.row * 2 * hidden + c;
+      float u[8], v[8];
+      unpack8(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src)), u);
+      unpack8(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + hidden)), v);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        o[i] = u[i] * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-u[i] * kLog2e)) * v[i];
+    }
+    u32x2 q;
+    const uint32_t byte = quantize_block(o, q);
+    if (in) *reinterpret_cast<u32x2*>(g8 + at.row * hidden + c) = q;
+    if (at.valid()) store_scale(gs + at.row * pitch, at.block, at.blocks, pitch, byte, lane);
+  }
+}
+
+bool bad16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) != 0; }
+int status(int launch_rc) { return launch_rc == 0 ? AERIS_OK : AERIS_ERR_HIP_LAUNCH; }
+
+// Calls f(Const<K>) for the vectors of eight channels per lane that hold a row.
+template <typename F>
+void with_vectors(int channels, F&& f) {
+  const int v = (channels / 8 + 63) / 64;
+  if (v <= 1) f(Const<1>{});
+  else if (v <= 2) f(Const<2>{});
+  else if (v <= 4) f(Const<4>{});
+  else f(Const<8>{});
+}
+
+}  // namespace
+
+int fp8_check(int64_t n_rows, int64_t cols) {
+  if (n_rows <= 0 || cols < 64 || cols > AERIS_MAX_FP8_COLUMNS) return AERIS_ERR_INVALID_SHAPE;
+  if (cols % 64 != 0) return AERIS_ERR_NOT_DIVISIBLE;
+  // 64-bit products of a row and a workgroup number, byte offsets of rows
+  if (n_rows >= (1LL << 40)) return AERIS_ERR_INVALID_SHAPE;
+  return AERIS_OK;
+}
+
+int launch_fp8_quantize_rows(const void* x, bool f32, long long n_rows, int cols, unsigned char* x8,
+                             unsigned char* xs, hipStream_t stream) {
+  const dim3 grid(walk_grid(n_rows, cols));
+  return f32 ? launch_kernel(fp8_quantize_rows_kernel<float>, grid, dim3(kThreads256), 0, stream,
+                             static_cast<const float*>(x), n_rows, cols, x8, xs)
+             : launch_kernel(fp8_quantize_rows_kernel<bf16_t>, grid, dim3(kThreads256), 0, stream,
+                             static_cast<const bf16_t*>(x), n_rows, cols, x8, xs);
+}
+
+int launch_fp8_dequantize(const unsigned char* x8, const unsigned char* xs, long long n_rows, int cols, bf16_t* x,
+                          hipStream_t stream) {
+  return launch_kernel(fp8_dequantize_kernel, dim3(walk_grid(n_rows, cols)), dim3(kThreads256), 0, stream, x8, xs,
+                       n_rows, cols, x);
+}
+
+}  // namespace aeris
+
+using namespace aeris;
+
+extern "C" int32_t aeris_fp8_scale_pitch(int32_t cols) {
+  return fp8_check(1, cols) == AERIS_OK ? scale_pitch(cols) : 0;
+}
+
+extern "C" int aeris_fp8_quantize(const void* x, int32_t x_dtype, int64_t n_rows, int32_t channels, void* x8,
+                                  void* xs, void* xt8, void* xts, void* hip_stream) {
+  if (!x || (!x8 && !xt8) || !x8 != !xs || !xt8 != !xts) return AERIS_ERR_NULL_POINTER;
+  if (x_dtype != AERIS_DT_BF16 && x_dtype != AERIS_DT_F32) return AERIS_ERR_BAD_DTYPE;
+  if (const int rc = fp8_check(n_rows, channels)) return rc;
+  if (xt8)
+    if (const int rc = fp8_check(channels, n_rows)) return rc;
+  if (bad16(x) || bad16(x8) || bad16(xs) || bad16(xt8) || bad16(xts)) return AERIS_ERR_MISALIGNED;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  unsigned char *q = static_cast<unsigned char*>(x8), *qs = static_cast<unsigned char*>(xs);
+  if (!xt8) return status(launch_fp8_quantize_rows(x, x_dtype == AERIS_DT_F32, n_rows, channels, q, qs, st));
+  const dim3 grid((unsigned)((channels + AERIS_FP8_BLOCK - 1) / AERIS_FP8_BLOCK) *
+                  (unsigned)((n_rows + AERIS_FP8_BLOCK - 1) / AERIS_FP8_BLOCK));
+  unsigned char *t = static_cast<unsigned char*>(xt8), *ts = static_cast<unsigned char*>(xts);
+  return status(x_dtype == AERIS_DT_F32
+                    ? launch_kernel(fp8_quantize_transposed_kernel<float>, grid, dim3(kThreads256), 0, st,
+                                    static_cast<const float*>(x), (int)n_rows, channels, q, qs, t, ts)
+                    : launch_kernel(fp8_quantize_transposed_kernel<bf16_t>, grid, dim3(kThreads256), 0, st,
+                                    static_cast<const bf16_t*>(x), (int)n_rows, channels, q, qs, t, ts));
+}
+
+extern "C" int aeris_residual_norm_fp8_fwd(const void* x, const void* y, const float* alpha, const float* w,
+                                           const float* gamma, const float* beta, float eps, int64_t n_rows,
+                                           int64_t rows_per_sample, int32_t channels, void* s, float* r, void* h8,
+                                           void* hs, void* hip_stream) {
+  if (!x || !w || !gamma || !beta || !h8 || !hs || (y && (!alpha || !s))) return AERIS_ERR_NULL_POINTER;
+  if (const int rc = fp8_check(n_rows, channels)) return rc;
+  if (channels > AERIS_MAX_CHANNELS || rows_per_sample <= 0 || !(eps >= 0.f)) return AERIS_ERR_INVALID_SHAPE;
+  if (n_rows % rows_per_sample != 0) return AERIS_ERR_NOT_DIVISIBLE;
+  const int64_t n_samples = n_rows / rows_per_sample;
+  if (n_samples > (1 << 20)) return AERIS_ERR_INVALID_SHAPE;
+  if (bad16(x) || bad16(w) || bad16(gamma) || bad16(beta) || bad16(h8) || bad16(hs) ||
+      (y && (bad16(y) || bad16(alpha) || bad16(s))) || (reinterpret_cast<uintptr_t>(r) & 3))
+    return AERIS_ERR_MISALIGNED;
+  // about kTargetChunks workgroups in all, at least a row per wave in each
+  int64_t chunks = (kTargetChunks + n_samples - 1) / n_samples;
+  const int64_t most = (rows_per_sample + kRowWaves - 1) / kRowWaves;
+  if (chunks > most) chunks = most;
+  const NormParams p{static_cast<const bf16_t*>(x), static_cast<const bf16_t*>(y), alpha, w, gamma, beta, eps,
+                     (long long)rows_per_sample, (int)chunks, channels, static_cast<bf16_t*>(s), r,
+                     static_cast<unsigned char*>(h8), static_cast<unsigned char*>(hs)};
+  const dim3 grid((unsigned)(n_samples * chunks));
+  const size_t smem = (y ? 3 : 2) * sizeof(float) * channels;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  int rc = -1;
+  with_vectors(channels, [&](auto k) {
+    constexpr int K = decltype(k)::value;
+    rc = y ? launch_kernel(residual_norm_fp8_kernel<K, true>, grid, dim3(kThreads256), smem, st, p)
+           : launch_kernel(residual_norm_fp8_kernel<K, false>, grid, dim3(kThreads256), smem, st, p);
+  });
+  return status(rc);
+}
+
+extern "C" int aeris_swiglu_fp8_fwd(const void* uv, int64_t n_rows, int32_t hidden, void* g8, void* gs,
+                                    void* hip_stream) {
+  if (!uv || !g8 || !gs) return AERIS_ERR_NULL_POINTER;
+  if (const int rc = fp8_check(n_rows, hidden)) return rc;
+  if (bad16(uv) || bad16(g8) || bad16(gs)) return AERIS_ERR_MISALIGNED;
+  return status(launch_kernel(swiglu_fp8_kernel, dim3(walk_grid(n_rows, hidden)), dim3(kThreads256), 0,
+                              static_cast<hipStream_t>(hip_stream), static_cast<const bf16_t*>(uv),
+                              (long long)n_rows, hidden, static_cast<unsigned char*>(g8),
+                              static_cast<unsigned char*>(gs)));
+}

@@ -1,0 +1,18 @@
+// Quantised rows (fp8_rows.hip) as the products of them (fp8_linear.hip) use them.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "winattn_common.hpp"
+
+namespace aeris {
+
+// AERIS_OK if a quantised matrix may have this size, else an AERIS_ERR_ code.
+int fp8_check(int64_t n_rows, int64_t cols);
+// 0 on success, -1 if the launch failed.
+int launch_fp8_quantize_rows(const void* x, bool f32, long long n_rows, int cols, unsigned char* x8,
+                             unsigned char* xs, hipStream_t stream);
+int launch_fp8_dequantize(const unsigned char* x8, const unsigned char* xs, long long n_rows, int cols, bf16_t* x,
+                          hipStream_t stream);
+
+}  // namespace aeris

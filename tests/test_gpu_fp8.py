@@ -1,0 +1,494 @@
+"""GPU parity of the 8-bit path (include/aeris_fp8.h) against oracle/fp8_oracle.py and oracle/block_oracle.py.
+
+Quantised bf16 and fp32 rows have to be the oracle's to the bit: a power-of-two scale is exact and e4m3 of it is
+one rounding.  Where a value is computed first (norm, gate) it carries fp32 errors into that rounding:
+  |q scale - h| <= 2^-4 |h| (half a step of e4m3) or 2^-10 scale (half its smallest) + 4e-6 of the terms of h,
+and a scale may be the neighbour of the oracle's only if the block's largest value lies within 4e-6 of the border.
+Products: the bf16 result is within 2^-8 of the value (half a step), and three errors of sums are added:
+  7 * 2^-13 * sum over groups of eight channels of the largest |x w| (what the matrix instruction drops, stated in
+  the header), bounded by the group's largest |x| times its largest |w|;
+  (channels / 32 + 8) * 2^-23 * sum |x w| (fp32 additions of the groups and steps, truncating ones included).
+"""
+import numpy as np
+import pytest
+import torch
+
+from oracle import block_oracle as bo
+from oracle import fp8_oracle as fo
+from paper_2509_13523_amd import binding as B
+from paper_2509_13523_amd import synth
+import parity_log
+
+pytestmark = pytest.mark.gpu
+
+SLACK = 4e-6            # of the sum of magnitudes of an element's terms: about 30 fp32 roundings of 2^-24 and the
+                        # hardware's reciprocal and exponential of one unit each
+
+
+def to_f64(t):
+    return t.double().cpu().numpy()
+
+
+def bf16(a):
+    """(device tensor, its values) of an array rounded to bf16."""
+    bits = synth.f32_to_bf16_bits(np.asarray(a, dtype=np.float32))
+    return torch.from_numpy(bits.view(np.int16)).cuda().view(torch.bfloat16), synth.bf16_bits_to_f64(bits)
+
+
+def f32(a):
+    a = np.asarray(a, dtype=np.float32)
+    return torch.from_numpy(a).cuda(), a.astype(np.float64)
+
+
+def codes(q, scales):
+    return q.view(torch.uint8).cpu().numpy(), scales.view(torch.uint8).cpu().numpy()
+
+
+def dev(q, scales):
+    return (torch.from_numpy(q).cuda().view(torch.float8_e4m3fn),
+            torch.from_numpy(scales).cuda().view(torch.float8_e8m0fnu))
+
+
+def same_codes(got, want):
+    """Equal but for the sign of NaN."""
+    nan = (want & 127) == 127
+    assert got.shape == want.shape and (got[~nan] == want[~nan]).all() and ((got[nan] & 127) == 127).all()
+
+
+def rows_with_gain(rng, n, c):
+    return rng.standard_normal((n, c)) * np.exp(rng.standard_normal(c))
+
+
+# ------------------------------------------------------------------------------------- quantise
+def hard_rows(rng, n, c, most):
+    """Rows with what a block can meet: zeros, one value alone, values at the border of a scale, values that are not
+    finite, and magnitudes from the smallest to the largest."""
+    x = rows_with_gain(rng, n, c)
+    for i in range(n):
+        kind, at = i % 9, rng.integers(c)
+        if kind == 1: x[i] = 0.0
+        elif kind == 2: x[i] = 0.0; x[i, at] = -3.0
+        elif kind == 3: x[i] = np.clip(x[i], -1, 1) * 100; x[i, at] = 448.0 * 2.0 ** (i % 7 - 3)
+        elif kind == 4: x[i, at] = np.inf; x[i, (at + 5) % c] = -np.inf; x[i, (at + 77) % c] = np.nan
+        elif kind == 5: x[i] *= 2.0 ** -120
+        elif kind == 6: x[i] *= most / np.abs(x[i]).max()
+        elif kind == 7: x[i] = np.nan
+        elif kind == 8: x[i] *= np.exp2(rng.integers(-20, 20, c))
+    return x
+
+
+@pytest.mark.parametrize("n,c,transposed", [
+    (1, 64, False), (1, 128, False), (3, 192, False), (17, 448, False), (200, 2048, False), (33, 5504, False),
+    (64, 64, True), (128, 128, True), (192, 320, True), (64, 1088, True), (1152, 192, True), (320, 512, True)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_quantize_is_the_oracle_to_the_bit(n, c, transposed, dtype):
+    rng = np.random.default_rng(100 * n + c)
+    t, x = (bf16 if dtype == "bf16" else f32)(hard_rows(rng, n, c, 3.3e38))
+    x8, xs, xt8, xts = B.aeris_fp8_quantize(t, transposed=transposed)
+    torch.cuda.synchronize()
+    got, want = codes(x8, xs), fo.quantize(x)
+    same_codes(got[0], want[0])
+    assert (got[1] == want[1]).all()
+    if not transposed:
+        assert xt8 is None and xts is None
+        return
+    got, want = codes(xt8, xts), fo.quantize(x.T)
+    same_codes(got[0], want[0])
+    assert (got[1] == want[1]).all()
+    none, none2, a, b = B.aeris_fp8_quantize(t, rows=False, transposed=True)
+    torch.cuda.synchronize()
+    assert none is None and none2 is None
+    assert torch.equal(a.view(torch.uint8), xt8.view(torch.uint8)) and torch.equal(b.view(torch.uint8), xts.view(torch.uint8))
+
+
+# ------------------------------------------------------------------------------------- computed values
+def close_quantized(name, got, h, mag):
+    """got: (codes, scales); h: what was quantised, in 64 bits; mag: sum of magnitudes of each value's terms."""
+    q, scales = got
+    n, c = h.shape
+    value = fo.dequantize(q, scales)
+    allow = np.maximum(2.0 ** -4 * np.abs(h), 2.0 ** -10 * fo.per_column(scales, c)) + 1.07 * SLACK * mag
+    err = np.abs(value - h)
+    parity_log.add(name, "e4m3", np.linalg.norm(err) / np.linalg.norm(h), err.max(), np.abs(h).max(), allow.max())
+    assert (err <= allow).all()
+    want = fo.quantize(h)[1]
+    blocks = -(-c // 128)
+    assert (scales[:, blocks:] == 127).all()
+    for b in range(blocks):
+        part = np.abs(h[:, b * 128:(b + 1) * 128])
+        off = scales[:, b].astype(int) - want[:, b].astype(int)
+        slack = (SLACK * mag[:, b * 128:(b + 1) * 128]).max(axis=1)
+        border = 448.0 * 2.0 ** (np.minimum(scales[:, b], want[:, b]) - 127.0)
+        assert ((off == 0) | ((np.abs(off) == 1) & (np.abs(part.max(axis=1) - border) <= slack))).all()
+
+
+@pytest.mark.parametrize("samples,rows,c,residual", [
+    (1, 1, 64, True), (1, 3, 128, False), (2, 5, 192, True), (3, 37, 320, False), (1, 130, 576, True),
+    (5, 9, 1088, True), (1, 70, 2048, True), (2, 33, 2112, False), (1, 20, 4096, True), (300, 1, 64, True)])
+def test_residual_norm(samples, rows, c, residual):
+    rng = np.random.default_rng(7 * c + rows)
+    n, eps = samples * rows, 1e-6
+    tx, x = bf16(rows_with_gain(rng, n, c))
+    ty, y = bf16(rows_with_gain(rng, n, c))
+    (tw, w), (ta, a), (tg, g), (tb, b) = [f32(v) for v in (
+        1 + 0.1 * rng.standard_normal(c), 0.8 * rng.standard_normal((samples, c)),
+        0.3 * rng.standard_normal((samples, c)), 0.5 * rng.standard_normal((samples, c)))]
+    s, r, h8, hs = B.aeris_residual_norm_fp8_fwd(tx, ty if residual else None, ta if residual else None, tw, tg, tb,
+                                                 eps, rows)
+    torch.cuda.synchronize()
+    if residual:
+        assert torch.equal(s.view(torch.int16), B.aeris_gate_residual_fwd(tx, ty, ta, rows).view(torch.int16))
+        exact = x + np.repeat(a, rows, 0) * y
+        # half a bf16 step, and one fp32 rounding of the sum before it (an ulp where it meets a border)
+        assert (np.abs(to_f64(s) - exact) <= 2.0 ** -8 * np.abs(exact) + 2.0 ** -23 * (np.abs(x) + np.abs(np.repeat(a, rows, 0) * y))).all()
+    else:
+        assert s is tx
+    _, r_apart = B.aeris_rmsnorm_adaln_fwd(s, tw, tg, tb, eps, rows)
+    assert torch.equal(r, r_apart)
+    h, _ = bo.rmsnorm_adaln_fwd(to_f64(s), w, g, b, eps, rows)
+    mag = np.abs(h - np.repeat(b, rows, 0)) + np.abs(np.repeat(b, rows, 0))
+    close_quantized("h", codes(h8, hs), h, mag)
+    s2, r2, h82, hs2 = B.aeris_residual_norm_fp8_fwd(tx, ty if residual else None, ta if residual else None, tw, tg,
+                                                     tb, eps, rows, want_r=False)
+    torch.cuda.synchronize()
+    assert r2 is None and torch.equal(h8.view(torch.uint8), h82.view(torch.uint8))
+    assert torch.equal(hs.view(torch.uint8), hs2.view(torch.uint8))
+
+
+@pytest.mark.parametrize("c", [192, 1024])
+def test_residual_norm_in_place(c):
+    rng = np.random.default_rng(c)
+    n = 45
+    tx, _ = bf16(rows_with_gain(rng, n, c))
+    ty, _ = bf16(rows_with_gain(rng, n, c))
+    ta, tw, tg, tb = [f32(rng.standard_normal(v))[0] for v in ((1, c), c, (1, c), (1, c))]
+    s, r, h8, hs = B.aeris_residual_norm_fp8_fwd(tx, ty, ta, tw, tg, tb, 1e-6, n)
+    for which in (0, 1):
+        pair = [tx.clone(), ty.clone()]
+        s2, r2, h82, hs2 = B.aeris_residual_norm_fp8_fwd(*pair, ta, tw, tg, tb, 1e-6, n, s=pair[which])
+        torch.cuda.synchronize()
+        assert s2 is pair[which]
+        for p, q in ((s, s2), (r, r2), (h8, h82), (hs, hs2)):
+            assert torch.equal(p.view(torch.uint8), q.view(torch.uint8))
+        assert torch.equal(pair[1 - which], (tx, ty)[1 - which])
+
+
+def test_residual_norm_rows_that_are_not_finite_stay_alone():
+    rng = np.random.default_rng(2)
+    n, c = 12, 320
+    x = rows_with_gain(rng, n, c)
+    x[3, 7], x[8, 200], x[10] = np.inf, np.nan, 0.0
+    tx, _ = bf16(x)
+    tw, tg, tb = [f32(rng.standard_normal(v))[0] for v in (c, (1, c), (1, c))]
+    _, r, h8, hs = B.aeris_residual_norm_fp8_fwd(tx, None, None, tw, tg, tb, 1e-6, n)
+    torch.cuda.synchronize()
+    value = fo.dequantize(*codes(h8, hs))
+    assert np.isnan(value[8]).all() and np.isnan(value[3, 7])
+    fine = [i for i in range(n) if i not in (3, 8)]
+    assert np.isfinite(value[fine]).all()
+    assert np.allclose(value[10], fo.round_trip(to_f64(tb))[0])            # a row of zeros: beta
+
+
+@pytest.mark.parametrize("n,hidden", [(1, 64), (2, 128), (5, 192), (61, 576), (300, 1344), (40, 5504)])
+def test_swiglu(n, hidden):
+    rng = np.random.default_rng(hidden + n)
+    uv = rows_with_gain(rng, n, 2 * hidden)
+    uv[0, :8] = [0.0, -0.0, 90.0, -90.0, 300.0, -300.0, 1e-30, -1e-30]
+    t, v = bf16(uv)
+    g8, gs = B.aeris_swiglu_fp8_fwd(t)
+    torch.cuda.synchronize()
+    g = bo.swiglu_fwd(v)
+    close_quantized("g", codes(g8, gs), g, np.abs(g))
+
+
+# ------------------------------------------------------------------------------------- projection
+def operand(rng, n, c):
+    """A quantised matrix as (device pair, values)."""
+    q, scales = fo.quantize(rows_with_gain(rng, n, c))
+    return dev(q, scales), fo.dequantize(q, scales)
+
+
+def product_slack(x, w):
+    """What the sums of x w^T may be off by, see the head of this file."""
+    c = x.shape[1]
+    groups = lambda a: np.abs(a).reshape(a.shape[0], c // 8, 8).max(axis=2)
+    return 7 * 2.0 ** -13 * (groups(x) @ groups(w).T) + (c / 32 + 8) * 2.0 ** -23 * (np.abs(x) @ np.abs(w).T)
+
+
+def close_product(name, got, x, w):
+    ref, slack = fo.linear_fwd(x, w), product_slack(x, w)
+    got = to_f64(got)
+    err = np.abs(got - ref)
+    allow = 2.0 ** -8 * np.abs(ref) + 1.01 * slack + 1e-30
+    rel = np.linalg.norm(err) / np.linalg.norm(ref)
+    parity_log.add(name, "bf16", rel, err.max(), np.abs(ref).max(), allow.max())
+    assert np.isfinite(got).all() and (err <= allow).all()
+    if ref.size >= 4096:
+        assert rel <= 3e-3      # output rounding alone is 2^-9 / sqrt 3 * (up to 2, by the mantissa) = 1.7e-3
+
+
+SIZES = [
+    # rows, channels, out features
+    (1, 64, 64), (1, 2048, 192), (1, 192, 1088), (3, 128, 64), (15, 320, 128), (16, 576, 320), (17, 512, 64),
+    (31, 1024, 256), (33, 64, 448), (48, 640, 192), (63, 704, 64), (64, 128, 128), (65, 2112, 64), (127, 192, 192),
+    (128, 256, 576), (129, 1088, 320), (257, 128, 1600), (1000, 64, 2048), (700, 448, 4160), (4100, 192, 1088),
+    (2500, 1600, 2112),
+]
+
+
+@pytest.mark.parametrize("n,c,f", SIZES)
+def test_linear(n, c, f):
+    rng = np.random.default_rng(n + 3 * c + 7 * f)
+    (x8, xs), x = operand(rng, n, c)
+    (w8, ws), w = operand(rng, f, c)
+    guard = torch.full((n + 2, f), 123.0, dtype=torch.bfloat16, device="cuda")
+    y = B.aeris_linear_fp8_fwd(x8, xs, w8, ws, y=guard[1:n + 1])
+    torch.cuda.synchronize()
+    close_product("y", y, x, w)
+    assert (guard[0] == 123).all() and (guard[n + 1] == 123).all()       # rows beside the output are left as they were
+    again = B.aeris_linear_fp8_fwd(x8, xs, w8, ws)
+    torch.cuda.synchronize()
+    assert torch.equal(y.view(torch.int16), again.view(torch.int16))
+
+
+@pytest.mark.parametrize("n", [2, 40, 300, 3000])
+def test_linear_applies_each_block_its_scale(n):
+    """Blocks of very unlike scales; whole numbers whose sums fp32 holds, so the result is exact before its rounding."""
+    rng = np.random.default_rng(n)
+    c, f = 1216, 192
+    q = lambda rows: fo.encode(rng.integers(-8, 9, (rows, c)).astype(float))
+    scales = lambda rows: np.concatenate([rng.integers(124, 131, (rows, 10)), np.full((rows, 2), 127)], 1).astype(np.uint8)
+    xq, xs, wq, ws = q(n), scales(n), q(f), scales(f)
+    y = B.aeris_linear_fp8_fwd(*dev(xq, xs), *dev(wq, ws))
+    torch.cuda.synchronize()
+    ref = fo.linear_fwd(fo.dequantize(xq, xs), fo.dequantize(wq, ws))     # multiples of 2^-6, below 2^18: exact
+    want = torch.from_numpy(ref).float().bfloat16()
+    assert torch.equal(y.cpu().view(torch.int16), want.view(torch.int16))
+
+
+@pytest.mark.parametrize("n,c,f", [(5, 192, 64), (100, 704, 192), (600, 320, 1088)])
+def test_linear_keeps_nan_to_its_rows_and_features(n, c, f):
+    rng = np.random.default_rng(9)
+    xq, xs = fo.quantize(rows_with_gain(rng, n, c))
+    wq, ws = fo.quantize(rows_with_gain(rng, f, c))
+    xq[n // 2, c - 1], wq[f // 3, 0], xs[n - 1, 0] = 0x7f, 0xff, 127 + 100
+    y = to_f64(B.aeris_linear_fp8_fwd(*dev(xq, xs), *dev(wq, ws)))
+    bad = np.isnan(y)
+    assert bad[n // 2].all() and bad[:, f // 3].all()
+    bad[n // 2], bad[:, f // 3] = False, False
+    assert not bad.any()
+
+
+@pytest.mark.parametrize("n,c,f", [(1, 64, 64), (40, 128, 192), (64, 2048, 64), (131, 192, 576), (1000, 576, 320),
+                                   (2125, 64, 128), (1100, 1088, 1600)])
+def test_linear_bwd(n, c, f):
+    rng = np.random.default_rng(n + c + f)
+    (x8, xs), x = operand(rng, n, c)
+    tw, w = bf16(rng.standard_normal((f, c)) / np.sqrt(c))
+    _, _, wt8, wts = B.aeris_fp8_quantize(tw, rows=False, transposed=True)
+    tdy, dy = bf16(rows_with_gain(rng, n, f))
+    dx, dw = B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, tdy)
+    torch.cuda.synchronize()
+    wt = fo.dequantize(*codes(wt8, wts))
+    close_product("dx", dx, fo.round_trip(dy), wt)
+    # dW: the values are exact in bf16, so it is the gradient of a bf16 projection of them to the bit
+    _, want = B.aeris_linear_bwd(torch.from_numpy(x).cuda().bfloat16(), tw, tdy, want_dx=False)
+    assert torch.equal(dw, want)
+    err, mag = np.abs(to_f64(dw) - dy.T @ x), np.abs(dy).T @ np.abs(x)
+    assert (err <= max(1e-5, 4.0 * np.sqrt(n) * 2.0 ** -24) * mag).all()
+    # each alone, without the other's operands
+    dx2, none = B.aeris_linear_fp8_bwd(None, None, wt8, wts, tdy, want_dweight=False)
+    none2, dw2 = B.aeris_linear_fp8_bwd(x8, xs, None, None, tdy, want_dx=False)
+    torch.cuda.synchronize()
+    assert none is None and none2 is None
+    assert torch.equal(dx.view(torch.int16), dx2.view(torch.int16)) and torch.equal(dw, dw2)
+
+
+def test_linear_gradients_against_differences():
+    """Sums of y dy along two directions of the quantised operands, from the library's own forward products: y is
+    linear in each operand, so a difference is exact up to the rounding of y (2^-8 of each |y dy|)."""
+    rng = np.random.default_rng(31)
+    n, c, f = 96, 256, 192
+    (x8, xs), x = operand(rng, n, c)
+    (u8, us), u = operand(rng, n, c)
+    tw, _ = bf16(rng.standard_normal((f, c)) / 16.0)
+    tv, _ = bf16(rng.standard_normal((f, c)) / 16.0)
+    w8, ws, wt8, wts = B.aeris_fp8_quantize(tw, transposed=True)
+    v8, vs, _, _ = B.aeris_fp8_quantize(tv)
+    tdy, dy = bf16(fo.round_trip(rng.standard_normal((n, f))))            # quantising it again changes nothing
+    dx, dw = B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, tdy)
+    w, v = fo.dequantize(*codes(w8, ws)), fo.dequantize(*codes(v8, vs))
+    # the transposed weight is quantised along the other side: equal where no value fell below the range of its block
+    assert (fo.dequantize(*codes(wt8, wts)).T == w).mean() > 0.99
+    for (a8, a_s, b8, b_s), inner in (((u8, us, w8, ws), (to_f64(dx) * u).sum()),
+                                      ((x8, xs, v8, vs), (to_f64(dw) * v).sum())):
+        y = to_f64(B.aeris_linear_fp8_fwd(a8, a_s, b8, b_s))
+        assert abs((y * dy).sum() - inner) <= 2.0 ** -8 * (np.abs(y) * np.abs(dy)).sum() + 2.0 ** -8 * (np.abs(to_f64(dx) * u)).sum()
+
+
+# ------------------------------------------------------------------------------------- used together
+def feed_forward(t, rows):
+    """The feed-forward half of a layer, forward and backward, as a training step runs it."""
+    s, r, h8, hs = B.aeris_residual_norm_fp8_fwd(t["x"], t["y"], t["alpha"], t["w"], t["gamma"], t["beta"], 1e-6, rows)
+    up8, ups, upt8, upts = B.aeris_fp8_quantize(t["up"], transposed=True)
+    down8, downs, downt8, downts = B.aeris_fp8_quantize(t["down"], transposed=True)
+    uv = B.aeris_linear_fp8_fwd(h8, hs, up8, ups)
+    g8, gs = B.aeris_swiglu_fp8_fwd(uv)
+    out = B.aeris_linear_fp8_fwd(g8, gs, down8, downs)
+    dg, ddown = B.aeris_linear_fp8_bwd(g8, gs, downt8, downts, t["dout"])
+    duv = B.aeris_swiglu_bwd(uv, dg)
+    dh, dup = B.aeris_linear_fp8_bwd(h8, hs, upt8, upts, duv)
+    ds, dw, dgamma, dbeta = B.aeris_rmsnorm_adaln_bwd(s, t["w"], t["gamma"], r, dh, rows, dres=t["ds"])
+    dy, dalpha = B.aeris_gate_residual_bwd(t["y"], t["alpha"], ds, rows)
+    return dict(s=s, r=r, uv=uv, out=out, ddown=ddown, dup=dup, dx=ds, dy=dy, dw=dw, dgamma=dgamma, dbeta=dbeta,
+                dalpha=dalpha, dg=dg, duv=duv, dh=dh, h=(h8, hs), g=(g8, gs), up8=(up8, ups), upt8=(upt8, upts),
+                down8=(down8, downs), downt8=(downt8, downts))
+
+
+def same_bits(a, b):
+    return all(same_bits(p, q) for p, q in zip(a, b)) if isinstance(a, tuple) else torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
+def feed_forward_inputs(rng, samples, rows, c, hidden):
+    n = samples * rows
+    arrays = dict(x=rows_with_gain(rng, n, c), y=rng.standard_normal((n, c)), dout=rng.standard_normal((n, c)),
+                  ds=rng.standard_normal((n, c)), up=rng.standard_normal((2 * hidden, c)) / np.sqrt(c),
+                  down=rng.standard_normal((c, hidden)) / np.sqrt(hidden))
+    t = {k: bf16(v) for k, v in arrays.items()}
+    t.update(w=f32(1 + 0.1 * rng.standard_normal(c)), alpha=f32(0.8 * rng.standard_normal((samples, c))),
+             gamma=f32(0.3 * rng.standard_normal((samples, c))), beta=f32(0.5 * rng.standard_normal((samples, c))))
+    return {k: v[0] for k, v in t.items()}, {k: v[1] for k, v in t.items()}
+
+
+def test_feed_forward_half_of_a_layer():
+    """Against the chain in 64 bits with the same roundings to 8 bits (straight through in the backward pass).
+
+    How far the two may be apart.  A relative difference d in front of a rounding to 8 bits (steps of 1/16 to 1/8 of
+    the value, 0.09 in the mean) moves a value by a step with the probability d * 0.8 / 0.09, so the quantised values
+    differ by sqrt(0.072 d) in the mean.  s is rounded to bf16 here and not there: d = 1.7e-3, so h8 and with it uv
+    differ by 1.1e-2.  The gate has two such factors: 1.6e-2 in front of g8, behind it sqrt(0.072 * 1.6e-2) = 3.4e-2
+    (out, ddown).  duv has uv's difference twice or less, so its quantised form, dh and the sums over dh (dw, dgamma,
+    dbeta, dx, dy, dalpha) differ by 3.4e-2 too.  Allowed is twice that; uv alone 2.2e-2, s and r 3.4e-3."""
+    rng = np.random.default_rng(41)
+    samples, rows, c, hidden = 2, 150, 256, 704
+    t, a = feed_forward_inputs(rng, samples, rows, c, hidden)
+    got = feed_forward(t, rows)
+    torch.cuda.synchronize()
+    ref = {}
+    ref["s"] = bo.gate_residual_fwd(a["x"], a["y"], a["alpha"], rows)
+    h, ref["r"] = bo.rmsnorm_adaln_fwd(ref["s"], a["w"], a["gamma"], a["beta"], 1e-6, rows)
+    h = fo.round_trip(h)
+    ref["uv"] = fo.linear_fwd(h, fo.round_trip(a["up"]))
+    g = fo.round_trip(bo.swiglu_fwd(ref["uv"]))
+    ref["out"] = fo.linear_fwd(g, fo.round_trip(a["down"]))
+    dg, ref["ddown"] = fo.linear_bwd(g, fo.round_trip(a["down"].T), a["dout"])
+    duv = bo.swiglu_bwd(ref["uv"], dg)
+    dh, ref["dup"] = fo.linear_bwd(h, fo.round_trip(a["up"].T), duv)
+    ref["dx"], ref["dw"], ref["dgamma"], ref["dbeta"] = bo.rmsnorm_adaln_bwd_residual(
+        ref["s"], a["w"], a["gamma"], a["beta"], 1e-6, rows, dh, a["ds"])
+    _, ref["dy"], ref["dalpha"] = bo.gate_residual_bwd(a["y"], a["alpha"], ref["dx"], rows)
+    for name in ref:
+        x, want = to_f64(got[name]), ref[name]
+        rel = np.linalg.norm(x - want) / np.linalg.norm(want)
+        allow = dict(s=3.4e-3, r=3.4e-3, uv=2.2e-2).get(name, 6.8e-2)
+        parity_log.add(name, "", rel, np.abs(x - want).max(), np.abs(want).max(), allow)
+        assert rel <= allow, name
+
+
+def test_stages_of_the_feed_forward_half():
+    """Each stage from the operands that the stage before it left, to the bounds of the single calls."""
+    rng = np.random.default_rng(41)
+    samples, rows, c, hidden = 2, 150, 256, 704
+    t, a = feed_forward_inputs(rng, samples, rows, c, hidden)
+    got = feed_forward(t, rows)
+    torch.cuda.synchronize()
+    held = lambda name: fo.dequantize(*codes(*got[name]))
+    v = {k: to_f64(got[k]) for k in ("s", "uv", "dg", "duv")}
+    h, _ = bo.rmsnorm_adaln_fwd(v["s"], a["w"], a["gamma"], a["beta"], 1e-6, rows)
+    beta = np.abs(np.repeat(a["beta"], rows, 0))
+    close_quantized("h", codes(*got["h"]), h, np.abs(h) + 2 * beta)
+    close_product("uv", got["uv"], held("h"), held("up8"))
+    g = bo.swiglu_fwd(v["uv"])
+    close_quantized("g", codes(*got["g"]), g, np.abs(g))
+    close_product("out", got["out"], held("g"), held("down8"))
+    close_product("dg", got["dg"], fo.round_trip(a["dout"]), held("downt8"))
+    close_product("dh", got["dh"], fo.round_trip(v["duv"]), held("upt8"))
+    for name, dy, x in (("ddown", a["dout"], held("g")), ("dup", v["duv"], held("h"))):
+        assert (np.abs(to_f64(got[name]) - dy.T @ x) <= 1e-5 * np.abs(dy).T @ np.abs(x)).all()
+
+
+def test_captured_and_replayed_beside_eager_calls():
+    """The whole half in a HIP graph: replays with new inputs in place, eager work on other inputs between them."""
+    rng = np.random.default_rng(43)
+    rows, c, hidden = 90, 192, 320
+    sets = [feed_forward_inputs(rng, 1, rows, c, hidden)[0] for _ in range(3)]
+    want = [feed_forward(t, rows) for t in sets]
+    held = {k: v.clone() for k, v in sets[0].items()}
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        feed_forward(held, rows)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = feed_forward(held, rows)
+    for i in (1, 0, 2, 1):
+        for k in held:
+            held[k].copy_(sets[i][k])
+        graph.replay()
+        feed_forward(sets[(i + 1) % 3], rows)
+        torch.cuda.synchronize()
+        for k in got:
+            assert same_bits(got[k], want[i][k]), k
+
+
+def test_calls_on_two_streams_at_once():
+    rng = np.random.default_rng(47)
+    rows, c, hidden = 200, 256, 448
+    sets = [feed_forward_inputs(rng, 1, rows, c, hidden)[0] for _ in range(2)]
+    want = [feed_forward(t, rows) for t in sets]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    got = [[], []]
+    for _ in range(3):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                got[i].append(feed_forward(sets[i], rows))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for g in got[i]:
+            for k in g:
+                assert same_bits(g[k], want[i][k]), k
+
+
+# ------------------------------------------------------------------------------------- refusals
+def test_errors_are_reported():
+    bf = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(B.AerisError) as e:
+        B.aeris_fp8_quantize(bf(8, 100))
+    assert e.value.code == -3
+    with pytest.raises(B.AerisError) as e:
+        B.aeris_fp8_quantize(bf(100, 64), transposed=True)
+    assert e.value.code == -3
+    with pytest.raises(B.AerisError) as e:
+        B.aeris_fp8_quantize(bf(64, 64), rows=False)
+    assert e.value.code == -1
+    with pytest.raises(B.AerisError) as e:
+        B.aeris_swiglu_fp8_fwd(bf(8, 144))
+    assert e.value.code == -3
+    z = torch.zeros
+    with pytest.raises(B.AerisError) as e:
+        B.aeris_residual_norm_fp8_fwd(bf(8, 64), bf(8, 64), None, z(64, device="cuda"), z(2, 64, device="cuda"),
+                                      z(2, 64, device="cuda"), 1e-6, 4)
+    assert e.value.code == -1
+    x8, xs, _, _ = B.aeris_fp8_quantize(bf(64, 128))
+    w8, ws, wt8, wts = B.aeris_fp8_quantize(bf(64, 64), transposed=True)
+    with pytest.raises(AssertionError):
+        B.aeris_linear_fp8_fwd(x8, xs, w8, ws)                        # 128 and 64 channels
+    with pytest.raises(AssertionError):
+        B.aeris_linear_fp8_fwd(x8, xs[:, :2].contiguous(), w8, ws)    # scales of another size
+    with pytest.raises(ValueError):
+        B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, bf(64, 64), want_dx=False, want_dweight=False)
+    with pytest.raises(B.AerisError) as e:
+        B.aeris_linear_fp8_bwd(w8, ws, wt8, wts, bf(64, 64), workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    assert e.value.code == -8
