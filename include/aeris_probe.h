@@ -52,6 +52,14 @@ int aeris_projection_plan(int64_t n_rows, int64_t rows_per_sample, int32_t chann
 int aeris_linear_bwd_plan(int64_t n_rows, int32_t channels, int32_t out_features, int32_t* tile,
                           int32_t* ranges, int32_t* steps);
 
+/*
+ * How aeris_linear_fp8_fwd computes a size it accepts (else its error code): *tile, the sides of the
+ * workgroup tiles (256, 128 or 64; 16 for a few rows: 16 features by all rows); *in_turn, whether the XCDs
+ * take the token tiles in turn (1) or contiguous ranges of all tiles (0).  Launches nothing.
+ */
+int aeris_linear_fp8_plan(int64_t n_rows, int32_t channels, int32_t out_features, int32_t* tile,
+                          int32_t* in_turn);
+
 #ifdef __cplusplus
 }
 #endif

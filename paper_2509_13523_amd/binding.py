@@ -34,7 +34,8 @@ EXPORTS = ("aeris_winattn_fwd", "aeris_winattn_bwd", "aeris_winattn_bwd_stages",
            "aeris_linear_bwd_workspace_bytes", "aeris_linear_bwd",
            # include/aeris_fp8.h
            "aeris_fp8_scale_pitch", "aeris_fp8_quantize", "aeris_residual_norm_fp8_fwd", "aeris_swiglu_fp8_fwd",
-           "aeris_linear_fp8_fwd", "aeris_linear_fp8_bwd_workspace_bytes", "aeris_linear_fp8_bwd")
+           "aeris_linear_fp8_fwd", "aeris_linear_fp8_bwd_workspace_bytes", "aeris_linear_fp8_bwd",
+           "aeris_linear_fp8_plan")
 
 
 class aeris_winattn_params(ctypes.Structure):
@@ -158,6 +159,8 @@ def load():
     lib.aeris_linear_bwd_workspace_bytes.restype = sz
     lib.aeris_linear_bwd.argtypes = [vp, vp, vp, i64, i32, i32, vp, vp, vp, sz, vp]
     lib.aeris_linear_bwd.restype = ctypes.c_int
+    lib.aeris_linear_fp8_plan.argtypes = [i64, i32, i32, pi32, pi32]
+    lib.aeris_linear_fp8_plan.restype = ctypes.c_int
     lib.aeris_fp8_scale_pitch.argtypes = [i32]
     lib.aeris_fp8_scale_pitch.restype = i32
     lib.aeris_fp8_quantize.argtypes = [vp, i32, i64, i32, vp, vp, vp, vp, vp]
@@ -844,6 +847,15 @@ def aeris_linear_fp8_fwd(x8, xs, w8, ws, y=None):
     if rc != 0:
         raise AerisError(rc, "aeris_linear_fp8_fwd")
     return y
+
+
+def aeris_linear_fp8_plan(n_rows, channels, out_features):
+    """(sides of a workgroup tile, 16 for a few rows; whether the XCDs take token tiles in turn)."""
+    out = [ctypes.c_int32() for _ in range(2)]
+    rc = load().aeris_linear_fp8_plan(n_rows, channels, out_features, *[ctypes.byref(v) for v in out])
+    if rc != 0:
+        raise AerisError(rc, "aeris_linear_fp8_plan")
+    return out[0].value, bool(out[1].value)
 
 
 def aeris_linear_fp8_bwd_workspace_bytes(n_rows, channels, out_features):

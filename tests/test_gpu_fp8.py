@@ -251,6 +251,44 @@ def test_linear(n, c, f):
     assert torch.equal(y.view(torch.int16), again.view(torch.int16))
 
 
+@pytest.mark.parametrize("n,c,f,plan", [
+    # a few rows: one, two and four blocks of 16; steps shared by eight waves, fewer steps than waves, half a last step
+    (1, 2048, 12288, (16, False)), (1, 1600, 64, (16, False)), (16, 5504, 192, (16, False)), (17, 64, 64, (16, False)),
+    (31, 1216, 320, (16, False)), (33, 448, 192, (16, False)), (64, 2112, 128, (16, False)),
+    (64, 2048, 11008, (64, False)),          # as few rows, but many features: tiles
+    (65, 2112, 64, (64, False)), (129, 1088, 320, (64, False)), (1000, 64, 2048, (64, False)),
+    (4100, 192, 1088, (128, False)), (2500, 1600, 2112, (128, False)),
+    # the largest tiles: two steps, and lengths that leave 0 to 3 steps in the last group of scales; last blocks of 128
+    # and of 64 channels; one tile per workgroup and several; both orders of tiles; rows and features past whole tiles
+    (16217, 256, 896, (256, True)), (16310, 192, 832, (256, True)), (26827, 192, 1664, (256, False)),
+    (8178, 320, 1920, (256, True)), (18458, 320, 1728, (256, False)), (11760, 384, 2112, (256, True)),
+    (8128, 448, 1984, (256, True)), (24740, 512, 960, (256, True)), (8085, 576, 2048, (256, True)),
+    (22383, 576, 1088, (256, True)), (24675, 576, 1088, (256, False)), (22105, 640, 1088, (256, True)),
+    (16473, 704, 1472, (256, True)),
+])
+def test_linear_by_its_plan(n, c, f, plan):
+    """Sizes that reach each way of computing the product; every row of a workgroup tile's ends is there."""
+    assert B.aeris_linear_fp8_plan(n, c, f) == plan
+    test_linear(n, c, f)
+
+
+@pytest.mark.parametrize("n,c,f", [(172801, 1216, 2112), (400000, 320, 960), (20011, 5504, 2048), (4608, 2048, 65536)])
+def test_linear_of_many_tiles_on_samples(n, c, f):
+    """Long walks over tiles: sampled rows and features, among them those where tiles meet and end."""
+    rng = np.random.default_rng(n)
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    x8, xs, _, _ = B.aeris_fp8_quantize(torch.randn(n, c, device="cuda", dtype=torch.bfloat16, generator=gen))
+    w8, ws, _, _ = B.aeris_fp8_quantize(torch.randn(f, c, device="cuda", generator=gen))
+    y = B.aeris_linear_fp8_fwd(x8, xs, w8, ws)
+    torch.cuda.synchronize()
+    assert B.aeris_linear_fp8_plan(n, c, f)[0] == 256
+    rows = np.unique(np.concatenate([[0, 1, 255, 256, n - 257, n - 256, n - 255, n - 2, n - 1], rng.integers(0, n, 40)]))
+    cols = np.unique(np.concatenate([[0, 63, 255, 256, f - 257, f - 256, f - 1], rng.integers(0, f, 40)]))
+    x = fo.dequantize(*codes(x8[rows], xs.view(torch.uint8)[rows].view(torch.float8_e8m0fnu)))
+    w = fo.dequantize(*codes(w8[cols], ws.view(torch.uint8)[cols].view(torch.float8_e8m0fnu)))
+    close_product("y", y[rows][:, cols], x, w)
+
+
 @pytest.mark.parametrize("n", [2, 40, 300, 3000])
 def test_linear_applies_each_block_its_scale(n):
     """Blocks of very unlike scales; whole numbers whose sums fp32 holds, so the result is exact before its rounding."""
@@ -415,6 +453,22 @@ def test_stages_of_the_feed_forward_half():
     close_product("dh", got["dh"], fo.round_trip(v["duv"]), held("upt8"))
     for name, dy, x in (("ddown", a["dout"], held("g")), ("dup", v["duv"], held("h"))):
         assert (np.abs(to_f64(got[name]) - dy.T @ x) <= 1e-5 * np.abs(dy).T @ np.abs(x)).all()
+
+
+@pytest.mark.parametrize("n,c,f", [(30000, 1216, 1088), (40, 1216, 192)])
+def test_linear_scales_in_other_shapes(n, c, f):
+    """As test_linear_applies_each_block_its_scale, for the largest tiles (groups of four scales) and a few rows."""
+    assert B.aeris_linear_fp8_plan(n, c, f)[0] == (256 if n == 30000 else 16)
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    whole = lambda rows: torch.randint(-8, 9, (rows, c), device="cuda", generator=gen)
+    powers = lambda rows: torch.cat([torch.randint(124, 131, (rows, 10), device="cuda", generator=gen),
+                                     torch.full((rows, 2), 127, device="cuda")], 1).to(torch.uint8)
+    xq, xs, wq, ws = whole(n), powers(n), whole(f), powers(f)
+    y = B.aeris_linear_fp8_fwd(xq.float().to(torch.float8_e4m3fn), xs.view(torch.float8_e8m0fnu),
+                               wq.float().to(torch.float8_e4m3fn), ws.view(torch.float8_e8m0fnu))
+    value = lambda q, s: q.double() * torch.exp2(s.double() - 127).repeat_interleave(128, 1)[:, :c]
+    want = value(xq, xs) @ value(wq, ws).t().contiguous()                # multiples of 2^-6, below 2^18: exact
+    assert torch.equal(y, want.float().bfloat16())
 
 
 def test_captured_and_replayed_beside_eager_calls():
