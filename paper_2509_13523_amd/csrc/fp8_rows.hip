@@ -19,7 +19,7 @@ namespace {
 
 constexpr int kThreads256 = 256;
 constexpr int kGroups = kThreads256 / kBlockLanes;   // blocks a workgroup works on side by side
-constexpr unsigned kMostBlocks = 8192;               // workgroups of a launch over blocks
+constexpr unsigned kMostBlocks = 1u << 22;           // workgroups of a launch over blocks
 
 // Blocks a workgroup's 16 groups of lanes walk over: all blocks of the rows [r0, r1), 16 apart.
 struct BlockWalk {
@@ -46,10 +46,11 @@ struct BlockWalk {
     }
   }
 };
-// Workgroups for such a walk: whole rows each, about four blocks per group of lanes.
-unsigned walk_grid(long long n_rows, int cols) {
+// Workgroups for such a walk: whole rows each, about `each` blocks per group of lanes.  Many short workgroups are faster
+// than few long ones (quantised rows, 172,800 x 2048: 187 us, 5.7 TB/s; 8192 workgroups 211, 2048 218).
+unsigned walk_grid(long long n_rows, int cols, int each) {
   const long long blocks = (cols + AERIS_FP8_BLOCK - 1) / AERIS_FP8_BLOCK;
-  const long long rows_each = (4 * kGroups + blocks - 1) / blocks;
+  const long long rows_each = (each * kGroups + blocks - 1) / blocks;
   const long long want = (n_rows + rows_each - 1) / rows_each;
   return (unsigned)(want < (long long)kMostBlocks ? want : (long long)kMostBlocks);
 }
@@ -225,7 +226,6 @@ __global__ __launch_bounds__(kThreads256) void fp8_dequantize_kernel(const unsig
 // registers between its sum of squares and its result.  The expressions are those of
 // aeris_gate_residual_fwd and aeris_rmsnorm_adaln_fwd, so that s and r have their bits.
 constexpr int kRowWaves = 4;
-constexpr int kTargetChunks = 2048;
 
 struct NormParams {
   const bf16_t* x;
@@ -248,7 +248,8 @@ __device__ __forceinline__ void unpack8(const u32x4& raw, float (&f)[8]) {
   }
 }
 
-template <int K, bool kResidual>
+// Rows of up to 128 or 256 channels take 16 or 32 lanes (L), so that a wave has several (172,800 rows x 128: 53 -> 28 us).
+template <int K, int L, bool kResidual>
 __global__ __launch_bounds__(kThreads256) void residual_norm_fp8_kernel(NormParams p) {
   extern __shared__ __align__(16) float lds_f[];
   const int C = p.C;
@@ -263,17 +264,21 @@ __global__ __launch_bounds__(kThreads256) void residual_norm_fp8_kernel(NormPara
     if (kResidual) a_lds[c] = p.alpha[(long long)sample * C + c];
   }
   __syncthreads();
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int kRows = 64 / L;                          // of a wave
+  const int lane = threadIdx.x & (L - 1), wave = threadIdx.x >> 6;
   const float inv_c = 1.f / (float)C;
   const int blocks = (C + AERIS_FP8_BLOCK - 1) / AERIS_FP8_BLOCK, pitch = scale_pitch(C);
-  for (long long row = r0 + wave; row < r1; row += kRowWaves) {
+  // every lane of a wave takes part in the sums and rotations
+  for (long long first = r0 + wave * kRows; first < r1; first += kRowWaves * kRows) {
+    const long long row = first + (L == 64 ? 0 : (threadIdx.x & 63) / L);
+    const bool valid = L == 64 || row < r1;
     const u32x4* src = reinterpret_cast<const u32x4*>(p.x + row * C);
     const u32x4* add = kResidual ? reinterpret_cast<const u32x4*>(p.y + row * C) : nullptr;
     u32x4 raw[K], more[K];
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int v = k * 64 + lane;
-      const bool in = v * 8 < C;
+      const bool in = valid && v * 8 < C;
       raw[k] = in ? __builtin_nontemporal_load(&src[v]) : u32x4{0, 0, 0, 0};
       if (kResidual) more[k] = in ? __builtin_nontemporal_load(&add[v]) : u32x4{0, 0, 0, 0};
     }
@@ -282,7 +287,7 @@ __global__ __launch_bounds__(kThreads256) void residual_norm_fp8_kernel(NormPara
 #pragma unroll
       for (int k = 0; k < K; ++k) {
         const int v = k * 64 + lane;
-        if (v * 8 < C) {
+        if (valid && v * 8 < C) {
           float f[8], g[8];
           unpack8(raw[k], f);
           unpack8(more[k], g);
@@ -307,13 +312,13 @@ __global__ __launch_bounds__(kThreads256) void residual_norm_fp8_kernel(NormPara
       for (int i = 0; i < 8; ++i) ss = __builtin_fmaf(f[i], f[i], ss);
     }
 #pragma unroll
-    for (int m = 32; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, 64);
+    for (int m = L / 2; m >= 1; m >>= 1) ss += __shfl_xor(ss, m, 64);
     const float r = 1.f / __builtin_sqrtf(ss * inv_c + p.eps);
-    if (p.r != nullptr && lane == 0) p.r[row] = r;
+    if (p.r != nullptr && lane == 0 && valid) p.r[row] = r;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
       const int v = k * 64 + lane;
-      const bool in = v * 8 < C;
+      const bool in = valid && v * 8 < C;
       float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
       if (in) {
         float f[8];
@@ -332,49 +337,79 @@ __global__ __launch_bounds__(kThreads256) void residual_norm_fp8_kernel(NormPara
       const uint32_t byte = quantize_block(o, q);
       if (in) __builtin_nontemporal_store(q, reinterpret_cast<u32x2*>(p.h8 + row * C) + v);
       const int block = v / kBlockLanes;
-      if (block < blocks) store_scale(p.hs + row * pitch, block, blocks, pitch, byte, lane);
+      if (valid && block < blocks) store_scale(p.hs + row * pitch, block, blocks, pitch, byte, lane);
     }
   }
 }
 
 // ---- SwiGLU gate ------------------------------------------------------------------------------------
+// Two blocks per group of lanes, read before either is worked on, and no more per workgroup: 172,800 rows x 5504 832 us,
+// 5.7 TB/s (one block at a time in 8192 workgroups 991; results that pass the caches like the rest 981).
+constexpr int kGateAhead = 2;
 __global__ __launch_bounds__(kThreads256) void swiglu_fp8_kernel(const bf16_t* __restrict__ uv, long long n_rows,
                                                                  int hidden, unsigned char* __restrict__ g8,
                                                                  unsigned char* __restrict__ gs) {
   const int lane = threadIdx.x & (kBlockLanes - 1), pitch = scale_pitch(hidden);
   BlockWalk at;
   at.init(n_rows, hidden);
-  for (; __any(at.valid()); at.step()) {
-    const int c = at.block * AERIS_FP8_BLOCK + lane * 8;
-    const bool in = at.valid() && c < hidden;
-    float o[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (in) {
-      const bf16_t* src = uv + at.row * 2 * hidden + c;
-      float u[8], v[8];
-      unpack8(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src)), u);
-      unpack8(__builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + hidden)), v);
+  constexpr int U = kGateAhead;
+  while (__any(at.valid())) {
+    u32x4 u[U], v[U];
+    long long row[U];
+    int block[U];
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        o[i] = u[i] * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-u[i] * kLog2e)) * v[i];
+    for (int i = 0; i < U; ++i) {
+      row[i] = at.row;
+      block[i] = at.block;
+      const int c = block[i] * AERIS_FP8_BLOCK + lane * 8;
+      u[i] = v[i] = u32x4{0, 0, 0, 0};
+      if (row[i] < at.end && c < hidden) {
+        const bf16_t* src = uv + row[i] * 2 * hidden + c;
+        u[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src));
+        v[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src + hidden));
+      }
+      at.step();
     }
-    u32x2 q;
-    const uint32_t byte = quantize_block(o, q);
-    if (in) *reinterpret_cast<u32x2*>(g8 + at.row * hidden + c) = q;
-    if (at.valid()) store_scale(gs + at.row * pitch, at.block, at.blocks, pitch, byte, lane);
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+      const int c = block[i] * AERIS_FP8_BLOCK + lane * 8;
+      const bool in = row[i] < at.end && c < hidden;
+      float uf[8], vf[8], o[8];
+      unpack8(u[i], uf);
+      unpack8(v[i], vf);
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        o[e] = uf[e] * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-uf[e] * kLog2e)) * vf[e];
+      u32x2 q;
+      const uint32_t byte = quantize_block(o, q);
+      if (in) __builtin_nontemporal_store(q, reinterpret_cast<u32x2*>(g8 + row[i] * hidden + c));
+      if (row[i] < at.end) store_scale(gs + row[i] * pitch, block[i], at.blocks, pitch, byte, lane);
+    }
   }
+}
+
+// Workgroups per sample, of two rows per wave and place (at most kMostBlocks in all, and one per sample).  172,800 rows
+// x 2048 with residual 417 us, 5.95 TB/s, in 2048 workgroups 499, 8192 478, one row each 407; but 3 x 5477 rows x 1600
+// 20.7 in rows of two, 22.3 of one.
+int64_t chunks_per_sample(int64_t n_samples, int64_t rows_per_sample, int channels) {
+  const int64_t rows = 2 * kRowWaves * (channels <= 128 ? 4 : channels <= 256 ? 2 : 1);
+  const int64_t chunks = (rows_per_sample + rows - 1) / rows, most = (kMostBlocks + n_samples - 1) / n_samples;
+  return chunks < most ? chunks : most;
 }
 
 bool bad16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) != 0; }
 int status(int launch_rc) { return launch_rc == 0 ? AERIS_OK : AERIS_ERR_HIP_LAUNCH; }
 
-// Calls f(Const<K>) for the vectors of eight channels per lane that hold a row.
+// Calls f(Const<K>, Const<L>): vectors of eight channels per lane that hold a row, lanes of a row.
 template <typename F>
-void with_vectors(int channels, F&& f) {
+void with_row_shape(int channels, F&& f) {
   const int v = (channels / 8 + 63) / 64;
-  if (v <= 1) f(Const<1>{});
-  else if (v <= 2) f(Const<2>{});
-  else if (v <= 4) f(Const<4>{});
-  else f(Const<8>{});
+  if (channels <= 128) f(Const<1>{}, Const<16>{});
+  else if (channels <= 256) f(Const<1>{}, Const<32>{});
+  else if (v <= 1) f(Const<1>{}, Const<64>{});
+  else if (v <= 2) f(Const<2>{}, Const<64>{});
+  else if (v <= 4) f(Const<4>{}, Const<64>{});
+  else f(Const<8>{}, Const<64>{});
 }
 
 }  // namespace
@@ -389,7 +424,7 @@ int fp8_check(int64_t n_rows, int64_t cols) {
 
 int launch_fp8_quantize_rows(const void* x, bool f32, long long n_rows, int cols, unsigned char* x8,
                              unsigned char* xs, hipStream_t stream) {
-  const dim3 grid(walk_grid(n_rows, cols));
+  const dim3 grid(walk_grid(n_rows, cols, 4));
   return f32 ? launch_kernel(fp8_quantize_rows_kernel<float>, grid, dim3(kThreads256), 0, stream,
                              static_cast<const float*>(x), n_rows, cols, x8, xs)
              : launch_kernel(fp8_quantize_rows_kernel<bf16_t>, grid, dim3(kThreads256), 0, stream,
@@ -398,7 +433,7 @@ int launch_fp8_quantize_rows(const void* x, bool f32, long long n_rows, int cols
 
 int launch_fp8_dequantize(const unsigned char* x8, const unsigned char* xs, long long n_rows, int cols, bf16_t* x,
                           hipStream_t stream) {
-  return launch_kernel(fp8_dequantize_kernel, dim3(walk_grid(n_rows, cols)), dim3(kThreads256), 0, stream, x8, xs,
+  return launch_kernel(fp8_dequantize_kernel, dim3(walk_grid(n_rows, cols, 4)), dim3(kThreads256), 0, stream, x8, xs,
                        n_rows, cols, x);
 }
 
@@ -444,10 +479,7 @@ extern "C" int aeris_residual_norm_fp8_fwd(const void* x, const void* y, const f
   if (bad16(x) || bad16(w) || bad16(gamma) || bad16(beta) || bad16(h8) || bad16(hs) ||
       (y && (bad16(y) || bad16(alpha) || bad16(s))) || (reinterpret_cast<uintptr_t>(r) & 3))
     return AERIS_ERR_MISALIGNED;
-  // about kTargetChunks workgroups in all, at least a row per wave in each
-  int64_t chunks = (kTargetChunks + n_samples - 1) / n_samples;
-  const int64_t most = (rows_per_sample + kRowWaves - 1) / kRowWaves;
-  if (chunks > most) chunks = most;
+  const int64_t chunks = chunks_per_sample(n_samples, rows_per_sample, channels);
   const NormParams p{static_cast<const bf16_t*>(x), static_cast<const bf16_t*>(y), alpha, w, gamma, beta, eps,
                      (long long)rows_per_sample, (int)chunks, channels, static_cast<bf16_t*>(s), r,
                      static_cast<unsigned char*>(h8), static_cast<unsigned char*>(hs)};
@@ -455,10 +487,10 @@ extern "C" int aeris_residual_norm_fp8_fwd(const void* x, const void* y, const f
   const size_t smem = (y ? 3 : 2) * sizeof(float) * channels;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   int rc = -1;
-  with_vectors(channels, [&](auto k) {
-    constexpr int K = decltype(k)::value;
-    rc = y ? launch_kernel(residual_norm_fp8_kernel<K, true>, grid, dim3(kThreads256), smem, st, p)
-           : launch_kernel(residual_norm_fp8_kernel<K, false>, grid, dim3(kThreads256), smem, st, p);
+  with_row_shape(channels, [&](auto k, auto lanes) {
+    constexpr int K = decltype(k)::value, L = decltype(lanes)::value;
+    rc = y ? launch_kernel(residual_norm_fp8_kernel<K, L, true>, grid, dim3(kThreads256), smem, st, p)
+           : launch_kernel(residual_norm_fp8_kernel<K, L, false>, grid, dim3(kThreads256), smem, st, p);
   });
   return status(rc);
 }
@@ -468,7 +500,7 @@ extern "C" int aeris_swiglu_fp8_fwd(const void* uv, int64_t n_rows, int32_t hidd
   if (!uv || !g8 || !gs) return AERIS_ERR_NULL_POINTER;
   if (const int rc = fp8_check(n_rows, hidden)) return rc;
   if (bad16(uv) || bad16(g8) || bad16(gs)) return AERIS_ERR_MISALIGNED;
-  return status(launch_kernel(swiglu_fp8_kernel, dim3(walk_grid(n_rows, hidden)), dim3(kThreads256), 0,
+  return status(launch_kernel(swiglu_fp8_kernel, dim3(walk_grid(n_rows, hidden, kGateAhead)), dim3(kThreads256), 0,
                               static_cast<hipStream_t>(hip_stream), static_cast<const bf16_t*>(uv),
                               (long long)n_rows, hidden, static_cast<unsigned char*>(g8),
                               static_cast<unsigned char*>(gs)));
