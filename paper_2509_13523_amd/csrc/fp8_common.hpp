@@ -46,18 +46,22 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t most) {
   const int b = (int)((most + 0x1fffffu) >> 23) - 8;
   return (uint32_t)(b > 1 ? b : 1);
 }
-// 1 / scale, exact: scale bytes are 1 ... 247.
-__device__ __forceinline__ float scale_inverse(uint32_t byte) { return __uint_as_float((254u - byte) << 23); }
+__device__ __forceinline__ float scale_value(uint32_t byte) { return __uint_as_float(byte << 23); }
 
-// Eight values over the scale as e4m3 (nearest even; the conversion turns what is not finite into NaN).
-__device__ __forceinline__ u32x2 pack_e4m3(const float (&v)[8], float inverse) {
-  u32x2 q;
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h] * inverse, v[4 * h + 1] * inverse, 0, false);
-    q[h] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(v[4 * h + 2] * inverse, v[4 * h + 3] * inverse, w, true);
-  }
-  return q;
+// Four values over a scale as e4m3, one rounding to nearest even; what is not finite becomes NaN.
+typedef short i16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint32_t pack4_e4m3(float a, float b, float c, float d, float scale) {
+  i16x2 q = {0, 0};
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, a, b, scale, false);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(q, c, d, scale, true);
+  return __builtin_bit_cast(uint32_t, q);
+}
+// The same of four bf16 values, two per register.
+__device__ __forceinline__ uint32_t pack4_e4m3(uint32_t ab, uint32_t cd, float scale) {
+  i16x2 q = {0, 0};
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, __builtin_bit_cast(bf16x2, ab), scale, false);
+  q = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(q, __builtin_bit_cast(bf16x2, cd), scale, true);
+  return __builtin_bit_cast(uint32_t, q);
 }
 
 // Quantises a block per 16 lanes; lanes without columns pass zeros.  Every lane of the wave takes part.
@@ -66,7 +70,8 @@ __device__ __forceinline__ uint32_t quantize_block(const float (&v)[8], u32x2& q
   uint32_t most = block_max(most8(v, false));
   if (__builtin_expect(__any(most >= kNotFinite), 0)) most = block_max(most8(v, true));
   const uint32_t byte = scale_byte(most);
-  q = pack_e4m3(v, scale_inverse(byte));
+  const float scale = scale_value(byte);
+  q = u32x2{pack4_e4m3(v[0], v[1], v[2], v[3], scale), pack4_e4m3(v[4], v[5], v[6], v[7], scale)};
   return byte;
 }
 
