@@ -775,19 +775,28 @@ def _empty_quantized(rows, cols, device):
             torch.empty((rows, -(-cols // 512) * 4), dtype=torch.float8_e8m0fnu, device=device))
 
 
+def _here(*tensors):
+    """All on the current device, whose stream the call takes."""
+    import torch
+    here = torch.cuda.current_device()
+    for t in tensors:
+        assert t is None or t.get_device() == here
+
+
 def _quantized(q, scales):
     import torch
-    assert q.is_cuda and q.is_contiguous() and q.dtype == torch.float8_e4m3fn and q.dim() == 2
-    assert scales.is_cuda and scales.is_contiguous() and scales.dtype == torch.float8_e8m0fnu
-    assert scales.shape == (q.shape[0], -(-q.shape[1] // 512) * 4)
-    return q.shape[0], q.shape[1]
+    n, c = q.shape
+    assert q.dtype == torch.float8_e4m3fn and scales.dtype == torch.float8_e8m0fnu
+    assert q.is_contiguous() and scales.is_contiguous() and scales.shape == (n, (c + 511) // 512 * 4)
+    return n, c
 
 
 def aeris_fp8_quantize(x, rows=True, transposed=False):
     """x [n, C] bf16 or fp32.  Returns (x8, xs, xt8, xts): x quantised by rows and its transpose
     quantised by rows; entries not asked for are None."""
     import torch
-    assert x.is_cuda and x.is_contiguous() and x.dim() == 2 and x.dtype in (torch.bfloat16, torch.float32)
+    assert x.is_contiguous() and x.dim() == 2 and x.dtype in (torch.bfloat16, torch.float32)
+    _here(x)
     n, c = x.shape
     x8, xs = _empty_quantized(n, c, x.device) if rows else (None, None)
     xt8, xts = _empty_quantized(c, n, x.device) if transposed else (None, None)
@@ -810,7 +819,13 @@ def aeris_residual_norm_fp8_fwd(x, y, alpha, w, gamma, beta, eps, rows_per_sampl
         assert _rows(y) == (n, c)
         if s is None:
             s = torch.empty_like(x)
-        assert _rows(s) == (n, c)
+        else:
+            assert _rows(s) == (n, c)
+    if rows_per_sample > 0 and n % rows_per_sample == 0:             # the call refuses other sizes
+        per_sample = n // rows_per_sample * c
+        assert w.numel() == c and gamma.numel() == beta.numel() == per_sample
+        assert y is None or alpha is None or alpha.numel() == per_sample
+    _here(x, y, alpha, w, gamma, beta, s)
     r = torch.empty(n, dtype=torch.float32, device=x.device) if want_r else None
     h8, hs = _empty_quantized(n, c, x.device)
     rc = load().aeris_residual_norm_fp8_fwd(x.data_ptr(), _ptr(y), _ptr(alpha), w.data_ptr(), gamma.data_ptr(),
@@ -826,6 +841,7 @@ def aeris_swiglu_fp8_fwd(uv):
     """(g8, gs): g = silu(u) * v for uv = [u | v], quantised."""
     n, c2 = _rows(uv)
     assert c2 % 2 == 0
+    _here(uv)
     g8, gs = _empty_quantized(n, c2 // 2, uv.device)
     rc = load().aeris_swiglu_fp8_fwd(uv.data_ptr(), n, c2 // 2, g8.data_ptr(), gs.data_ptr(), _stream())
     if rc != 0:
@@ -841,7 +857,9 @@ def aeris_linear_fp8_fwd(x8, xs, w8, ws, y=None):
     assert c == cw
     if y is None:
         y = torch.empty((n, f), dtype=torch.bfloat16, device=x8.device)
-    assert _rows(y) == (n, f)
+    else:
+        assert _rows(y) == (n, f)
+    _here(x8, xs, w8, ws, y)
     rc = load().aeris_linear_fp8_fwd(x8.data_ptr(), xs.data_ptr(), w8.data_ptr(), ws.data_ptr(), n, c, f,
                                      y.data_ptr(), _stream())
     if rc != 0:
@@ -886,6 +904,8 @@ def aeris_linear_fp8_bwd(x8, xs, wt8, wts, dy, want_dx=True, want_dweight=True, 
     if workspace is None:
         workspace = torch.empty(max(aeris_linear_fp8_bwd_workspace_bytes(n, c, f), 16), dtype=torch.uint8,
                                 device=dy.device)
+    assert workspace.is_contiguous()
+    _here(dy, dx, dweight, workspace, *((wt8, wts) if want_dx else ()), *((x8, xs) if want_dweight else ()))
     rc = load().aeris_linear_fp8_bwd(_ptr(x8) if want_dweight else None, _ptr(xs) if want_dweight else None,
                                      _ptr(wt8) if want_dx else None, _ptr(wts) if want_dx else None,
                                      dy.data_ptr(), n, c, f, dx.data_ptr() if want_dx else None,

@@ -740,8 +740,8 @@ int launch_linear(LinearParams p, hipStream_t stream) {
 int check_linear(int64_t n_rows, int32_t channels, int32_t features) {
   if (const int rc = fp8_check(n_rows, channels)) return rc;
   if (const int rc = fp8_check(n_rows, features)) return rc;
-  // a launch holds less than 2^32 threads, 256 per 128 x 128 tile
-  return (n_rows + 127) / 128 * ((features + 127) / 128) < (1LL << 24) ? AERIS_OK : AERIS_ERR_INVALID_SHAPE;
+  // a launch holds less than 2^32 threads, 128 per 64 x 64 tile
+  return (n_rows + 63) / 64 * (features / 64) < (1LL << 25) ? AERIS_OK : AERIS_ERR_INVALID_SHAPE;
 }
 
 bool bad16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) != 0; }

@@ -122,6 +122,14 @@ def test_linear_refuses():
     assert call(n=1 << 39, f=65536) == -2                       # more tiles than a launch holds
 
 
+@pytest.mark.parametrize("f", [64, 192, 65536])
+def test_linear_takes_as_many_tiles_as_a_launch_holds(f):
+    most = ((1 << 25) - 1) // (f // 64) * 64
+    assert B.aeris_linear_fp8_plan(most, 128, f)[0] in (64, 128, 256)
+    with pytest.raises(B.AerisError):
+        B.aeris_linear_fp8_plan(most + 1, 128, f)
+
+
 def test_linear_bwd_refuses_and_sizes_its_workspace():
     lib = B.load()
     n, c, f = 1000, 192, 320

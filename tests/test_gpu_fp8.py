@@ -546,3 +546,29 @@ def test_errors_are_reported():
     with pytest.raises(B.AerisError) as e:
         B.aeris_linear_fp8_bwd(w8, ws, wt8, wts, bf(64, 64), workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
     assert e.value.code == -8
+
+
+@pytest.mark.parametrize("change", ["w", "gamma", "beta", "alpha", "y", "s"])
+def test_residual_norm_refuses_operands_of_another_size(change):
+    rows = lambda n: torch.zeros(n, 64, dtype=torch.bfloat16, device="cuda")
+    z = lambda n: torch.zeros(n, 64, device="cuda")
+    k = dict(x=rows(8), y=rows(8), alpha=z(2), w=z(1), gamma=z(2), beta=z(2), eps=1e-6, rows_per_sample=4, s=rows(8))
+    B.aeris_residual_norm_fp8_fwd(**k)
+    k[change] = rows(4) if change in "ys" else torch.zeros(32, device="cuda") if change == "w" else z(1)
+    with pytest.raises(AssertionError):
+        B.aeris_residual_norm_fp8_fwd(**k)
+
+
+def test_linear_refuses_operands_of_another_place():
+    q = lambda n, c: B.aeris_fp8_quantize(torch.zeros(n, c, dtype=torch.bfloat16, device="cuda"))[:2]
+    (x8, xs), (w8, ws) = q(3, 64), q(64, 64)
+    for at in range(4):
+        args = [x8, xs, w8, ws]
+        args[at] = args[at].cpu()
+        with pytest.raises(AssertionError):
+            B.aeris_linear_fp8_fwd(*args)
+    with pytest.raises(AssertionError):
+        B.aeris_linear_fp8_fwd(x8, xs, w8, ws, y=torch.zeros(3, 128, dtype=torch.bfloat16, device="cuda"))
+    with pytest.raises(AssertionError):
+        B.aeris_linear_fp8_bwd(w8, ws, w8, ws, torch.zeros(64, 64, dtype=torch.bfloat16, device="cuda"),
+                               workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda")[::2])
