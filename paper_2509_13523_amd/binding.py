@@ -769,10 +769,10 @@ def aeris_fp8_scale_pitch(cols):
     return load().aeris_fp8_scale_pitch(cols)
 
 
-def _empty_quantized(rows, cols, device):
+def _empty_quantized(x, rows, cols):
     import torch
-    return (torch.empty((rows, cols), dtype=torch.float8_e4m3fn, device=device),
-            torch.empty((rows, -(-cols // 512) * 4), dtype=torch.float8_e8m0fnu, device=device))
+    return (x.new_empty((rows, cols), dtype=torch.float8_e4m3fn),
+            x.new_empty((rows, (cols + 511) // 512 * 4), dtype=torch.float8_e8m0fnu))
 
 
 def _here(*tensors):
@@ -798,8 +798,8 @@ def aeris_fp8_quantize(x, rows=True, transposed=False):
     assert x.is_contiguous() and x.dim() == 2 and x.dtype in (torch.bfloat16, torch.float32)
     _here(x)
     n, c = x.shape
-    x8, xs = _empty_quantized(n, c, x.device) if rows else (None, None)
-    xt8, xts = _empty_quantized(c, n, x.device) if transposed else (None, None)
+    x8, xs = _empty_quantized(x, n, c) if rows else (None, None)
+    xt8, xts = _empty_quantized(x, c, n) if transposed else (None, None)
     rc = load().aeris_fp8_quantize(x.data_ptr(), AERIS_DT_F32 if x.dtype == torch.float32 else AERIS_DT_BF16,
                                    n, c, _ptr(x8), _ptr(xs), _ptr(xt8), _ptr(xts), _stream())
     if rc != 0:
@@ -826,8 +826,8 @@ def aeris_residual_norm_fp8_fwd(x, y, alpha, w, gamma, beta, eps, rows_per_sampl
         assert w.numel() == c and gamma.numel() == beta.numel() == per_sample
         assert y is None or alpha is None or alpha.numel() == per_sample
     _here(x, y, alpha, w, gamma, beta, s)
-    r = torch.empty(n, dtype=torch.float32, device=x.device) if want_r else None
-    h8, hs = _empty_quantized(n, c, x.device)
+    r = x.new_empty(n, dtype=torch.float32) if want_r else None
+    h8, hs = _empty_quantized(x, n, c)
     rc = load().aeris_residual_norm_fp8_fwd(x.data_ptr(), _ptr(y), _ptr(alpha), w.data_ptr(), gamma.data_ptr(),
                                             beta.data_ptr(), float(eps), n, rows_per_sample, c,
                                             None if y is None else s.data_ptr(), _ptr(r), h8.data_ptr(),
@@ -842,7 +842,7 @@ def aeris_swiglu_fp8_fwd(uv):
     n, c2 = _rows(uv)
     assert c2 % 2 == 0
     _here(uv)
-    g8, gs = _empty_quantized(n, c2 // 2, uv.device)
+    g8, gs = _empty_quantized(uv, n, c2 // 2)
     rc = load().aeris_swiglu_fp8_fwd(uv.data_ptr(), n, c2 // 2, g8.data_ptr(), gs.data_ptr(), _stream())
     if rc != 0:
         raise AerisError(rc, "aeris_swiglu_fp8_fwd")
@@ -856,7 +856,7 @@ def aeris_linear_fp8_fwd(x8, xs, w8, ws, y=None):
     f, cw = _quantized(w8, ws)
     assert c == cw
     if y is None:
-        y = torch.empty((n, f), dtype=torch.bfloat16, device=x8.device)
+        y = x8.new_empty((n, f), dtype=torch.bfloat16)
     else:
         assert _rows(y) == (n, f)
     _here(x8, xs, w8, ws, y)
