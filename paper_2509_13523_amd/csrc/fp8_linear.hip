@@ -296,13 +296,15 @@ __global__ __launch_bounds__(Sh::kWaves * 64, 2) void fp8_linear_kernel(LinearPa
 // Scales: four bytes per row are those of four steps, so a group of four steps has one copy of 512 dwords, into one
 // of two buffers behind the operand stages.
 //
-// Bound by the results and by power: of a tile's 64,000 cycles at 2048 channels 16 steps take 2700 each (2048 of them
-// products, at 1.85 GHz under the board's cap), 8000 go into moving 256 accumulators of a lane to the vector
-// registers, rounding and storing them.  Moved among the products of the next phase instead they cost the same (they
-// wait for the matrix pipe), but for few channels: 20011 x 768 -> 2304 44 instead of 47 us.  Per call, us, eight
-// waves of two SIMD mates in turns (the scheme of the bf16 projections) / this: 172800 x 2048 -> 11008 3320 / 3240,
-// 172800 x 5504 -> 2048 1545 / 1480, 8192 x 8192 -> 8192 413 / 402; the vendor's product with one scale 3030, 1383,
-// 341.
+// Bound by the board's power cap and by the results.  172,800 x 2048 -> 11008 runs at 1.7 to 2.0 GHz with the matrix
+// pipe busy 59 % of a tile's 55,600 cycles: 16 steps take 2900 each (2048 of them products), 8000 go into moving 256
+// accumulators of a lane to the vector registers, rounding and storing them.  Moved among the products of the next
+// phase instead they cost the same (they wait for the matrix pipe); stores that pass the caches, or accumulators
+// cleared by the matrix pipe, gained nothing either.  Few channels are bound by the burst of results that all CUs
+// store at a time: 20,011 x 768 -> 2304 44 us (stores among products 47, past the caches 48), at 2.4 GHz.  Per call,
+// us, eight waves of two SIMD mates in turns (the scheme of the bf16 projections) / this: 172,800 x 2048 -> 11008
+// 3320 / 3200, 172,800 x 5504 -> 2048 1545 / 1480, 8192 x 8192 -> 8192 413 / 400; the vendor's product with one scale
+// 3030, 1383, 341.
 constexpr int kLargeSide = 256;
 constexpr int kLargeStage = 2 * kLargeSide * kStep;                  // bytes of a stage; XORed into LDS addresses
 constexpr int kLargeScales = 2 * kLargeStage, kLargeScaleBytes = 2 * kLargeSide * 4;
@@ -424,11 +426,13 @@ __global__ __launch_bounds__(256, 1) void fp8_linear_large_kernel(LinearParams p
     }
   };
 
-  // ---- operand reads: per lane two 16-byte chunks of a row, g and g + 4
+  // ---- operand reads: per lane two 16-byte chunks of a row, g' and g' + 4 with g' = 0, 3, 1, 2.  An LDS access takes
+  // the lanes 0 ... 3, 12 ... 15 and 20 ... 27 of a half together (rows 0 ... 3, 12 ... 15 at one g, 4 ... 11 at the
+  // next): with g' = g half of each collided, 15 % of a long product's cycles, though under the power cap not its time.
   uint32_t va[2], vb[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
-    const uint32_t off = li * 128 + (((g + 4 * j) ^ Sub::swz(li)) << 4);
+    const uint32_t off = li * 128 + ((((g >> 1) ^ (g & 1 ? 3 : 0)) + 4 * j) ^ Sub::swz(li)) * 16;
     va[j] = lds0 + wn * 16384 + off;
     vb[j] = lds0 + kLargeSide * kStep + wm * 16384 + off;
   }
