@@ -35,7 +35,7 @@ EXPORTS = ("aeris_winattn_fwd", "aeris_winattn_bwd", "aeris_winattn_bwd_stages",
            # include/aeris_fp8.h
            "aeris_fp8_scale_pitch", "aeris_fp8_quantize", "aeris_residual_norm_fp8_fwd", "aeris_swiglu_fp8_fwd",
            "aeris_linear_fp8_fwd", "aeris_linear_fp8_bwd_workspace_bytes", "aeris_linear_fp8_bwd",
-           "aeris_linear_fp8_plan")
+           "aeris_linear_fp8_plan", "aeris_linear_fp8_parts")
 
 
 class aeris_winattn_params(ctypes.Structure):
@@ -161,6 +161,8 @@ def load():
     lib.aeris_linear_bwd.restype = ctypes.c_int
     lib.aeris_linear_fp8_plan.argtypes = [i64, i32, i32, pi32, pi32]
     lib.aeris_linear_fp8_plan.restype = ctypes.c_int
+    lib.aeris_linear_fp8_parts.argtypes = [i64, i32, i32, pi32]
+    lib.aeris_linear_fp8_parts.restype = ctypes.c_int
     lib.aeris_fp8_scale_pitch.argtypes = [i32]
     lib.aeris_fp8_scale_pitch.restype = i32
     lib.aeris_fp8_quantize.argtypes = [vp, i32, i64, i32, vp, vp, vp, vp, vp]
@@ -874,6 +876,15 @@ def aeris_linear_fp8_plan(n_rows, channels, out_features):
     if rc != 0:
         raise AerisError(rc, "aeris_linear_fp8_plan")
     return out[0].value, bool(out[1].value)
+
+
+def aeris_linear_fp8_parts(n_rows, channels, out_features):
+    """Parts of the channels whose sums a workgroup adds."""
+    out = ctypes.c_int32()
+    rc = load().aeris_linear_fp8_parts(n_rows, channels, out_features, ctypes.byref(out))
+    if rc != 0:
+        raise AerisError(rc, "aeris_linear_fp8_parts")
+    return out.value
 
 
 def aeris_linear_fp8_bwd_workspace_bytes(n_rows, channels, out_features):

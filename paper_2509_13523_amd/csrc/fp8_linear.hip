@@ -57,6 +57,8 @@ struct LinearShape {
 using LinearLarge = LinearShape<2, 2, 4, 4, 2>;    // 256 x 256, one workgroup per CU
 using LinearMedium = LinearShape<2, 2, 2, 2, 2>;   // 128 x 128, two workgroups per CU
 using LinearSmall = LinearShape<2, 1, 1, 2, 4>;    // 64 x 64, two workgroups per CU, three stages in flight
+using LinearShared = LinearShape<2, 1, 1, 2, 2>;   // 64 x 64, kShared groups of waves share the channels
+constexpr int kShared = 4;
 
 // Where a workgroup's tile lies: two scalar registers, from which the rest is worked out where it is needed.
 template <class Sh>
@@ -179,8 +181,13 @@ __device__ __forceinline__ void linear_clear(f32x16 (&acc)[2][NB]) {
 
 // One workgroup per tile.  Rows past the end repeat the last valid row (never stored); where the channels end
 // in the middle of the last block, the copies of its second half repeat the first and are not multiplied.
-template <class Sh>
-__global__ __launch_bounds__(Sh::kWaves * 64, 2) void fp8_linear_kernel(LinearParams p) {
+// G groups of Sh::kWaves waves share the channels of the tile: each takes a contiguous part of the steps, with stages
+// of its own, and the first adds the others' sums to its own in their order.  For fewer tiles than CUs, where a step of
+// 64 x 64 is its instructions and latencies (0.5 us) and nothing else runs beside it: 128 rows x 5504 -> 2048 21.2 ->
+// 14.6 us, x 2048 -> 2048 10.1 -> 7.1, x 768 -> 2304 6.1 -> 5.5 (two groups with four stages each 14.9, 7.9, 5.5;
+// three with three 14.4, 7.9, 5.5).
+template <class Sh, int G>
+__global__ __launch_bounds__(Sh::kWaves * G * 64, 2) void fp8_linear_kernel(LinearParams p) {
   constexpr int kBN = Sh::kBN, NB = Sh::NB, W = Sh::kWaves, kStages = Sh::kStages;
   constexpr int kStageBytes = Sh::kStageBytes;
   // every wave copies 32 weight rows, 32 token rows and the scales of 64 rows of one operand
@@ -190,7 +197,8 @@ __global__ __launch_bounds__(Sh::kWaves * 64, 2) void fp8_linear_kernel(LinearPa
   LinearTileAt<Sh> at;
   linear_tile(p, blockIdx.x, at);
   const int tid = threadIdx.x;
-  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, group = __builtin_amdgcn_readfirstlane((tid >> 6) / W);
+  const int wave = __builtin_amdgcn_readfirstlane((tid >> 6) % W);
   const int wm = wave / Sh::WN, wn = wave % Sh::WN;
   const int li = lane & 31, g = lane >> 5;
   // ---- copies: instruction j moves rows 8j..8j+7 of the weight rows, then of the token rows; wave w
@@ -213,10 +221,11 @@ __global__ __launch_bounds__(Sh::kWaves * 64, 2) void fp8_linear_kernel(LinearPa
   const unsigned long long sbase = reinterpret_cast<unsigned long long>(
       of_w ? p.ws + (long long)at.f0() * p.pitch : p.xs + at.row0() * p.pitch);
 
-  const uint32_t lds0 = lds_address(smem);
+  const uint32_t lds0 = lds_address(smem) + (uint32_t)(group * Sh::kSmem);
   const int k_steps = (p.K + kStep - 1) / kStep;
+  const int begin = k_steps * group / G, end = k_steps * (group + 1) / G;
   auto copy_step = [&](uint32_t stage, int step) __attribute__((always_inline)) {
-    const uint32_t enable = step < k_steps, less = step == k_steps - 1 ? back : 0;
+    const uint32_t enable = step < end, less = step == k_steps - 1 ? back : 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       async_copy16_off(voff[i] - less, (i < 4 ? wbase : xbase) + (unsigned long long)step * kStep,
@@ -238,17 +247,19 @@ __global__ __launch_bounds__(Sh::kWaves * 64, 2) void fp8_linear_kernel(LinearPa
   linear_clear(acc);
 
 #pragma unroll
-  for (int st = 0; st < kStages - 1; ++st) copy_step(lds0 + st * kStageBytes, st);
+  for (int st = 0; st < kStages - 1; ++st) copy_step(lds0 + st * kStageBytes, begin + st);
   uint32_t here = 0;
-  for (int ks = 0; ks < k_steps; ++ks) {
+  const int most = (k_steps + G - 1) / G;              // steps of the longest part: all waves meet as often
+  for (int i = 0, ks = begin; i < most; ++i, ++ks) {
     // this wave's copies of this stage have landed; those of later stages, nine each, may be on their way
-    const int later = k_steps - 1 - ks;
+    const int later = end - 1 - ks;
     if (kStages >= 4 && later >= 2) asm volatile("s_waitcnt vmcnt(18)" ::: "memory");
-    else if (kStages >= 4 && later >= 1) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
+    else if (kStages >= 3 && later >= 1) asm volatile("s_waitcnt vmcnt(9)" ::: "memory");
     else wait_async_loads();
     __syncthreads();               // this stage has landed; every reader of the stage before is done
     const uint32_t next = here == 0 ? (kStages - 1) * kStageBytes : here - kStageBytes;
     copy_step(lds0 + next, ks + kStages - 1);
+    if (G > 1 && later < 0) break;                     // only ever in the last of all
     int scale_w[2], scale_x[NB];
 #pragma unroll
     for (int a = 0; a < 2; ++a) scale_w[a] = scale_at(sa + here + a * 128 + (ks & 3));
@@ -256,7 +267,7 @@ __global__ __launch_bounds__(Sh::kWaves * 64, 2) void fp8_linear_kernel(LinearPa
     for (int b = 0; b < NB; ++b) scale_x[b] = scale_at(sb + here + b * 128 + (ks & 3));
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
-      if (m == 1 && half && later == 0) break;
+      if (m == 1 && half && ks == k_steps - 1) break;
       i32x8 w[2], x[NB];
 #pragma unroll
       for (int a = 0; a < 2; ++a)
@@ -272,6 +283,32 @@ __global__ __launch_bounds__(Sh::kWaves * 64, 2) void fp8_linear_kernel(LinearPa
     here = here + kStageBytes == (uint32_t)Sh::kSmem ? 0 : here + kStageBytes;
   }
   __syncthreads();                 // every wave is done with the operand stages
+  if constexpr (G > 1) {
+    // the sums of the other groups, in their stages
+    const uint32_t part = lds_address(smem) + (uint32_t)(wave * (NB * 8192) + lane * 16);
+    auto each = [&](auto&& f) __attribute__((always_inline)) {
+#pragma unroll
+      for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) f(acc[a][b], q, (uint32_t)(((a * NB + b) * 4 + q) << 10));
+    };
+    if (group > 0)
+      each([&](const f32x16& c, int q, uint32_t off) __attribute__((always_inline)) {
+        *reinterpret_cast<AERIS_LDS f32x4*>(part + (uint32_t)(group * Sh::kSmem) + off) =
+            f32x4{c[4 * q], c[4 * q + 1], c[4 * q + 2], c[4 * q + 3]};
+      });
+    __syncthreads();
+    if (group > 0) return;
+#pragma unroll
+    for (int j = 1; j < G; ++j)
+      each([&](f32x16& c, int q, uint32_t off) __attribute__((always_inline)) {
+        const f32x4 v = *reinterpret_cast<const AERIS_LDS f32x4*>(part + (uint32_t)(j * Sh::kSmem) + off);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c[4 * q + e] += v[e];
+      });
+  }
   linear_store<Sh>(p, at, acc, lds0 + wave * (NB * 4096), wm, wn, lane);
 }
 
@@ -664,7 +701,7 @@ int launch_linear_rows(const LinearParams& p, hipStream_t stream) {
                           : launch_kernel(fp8_linear_rows_kernel<4>, grid, block, 0, stream, p);
 }
 
-template <class Sh>
+template <class Sh, int G = 1>
 int launch_linear_shape(LinearParams p, hipStream_t stream) {
   p.n_tiles = (p.F + Sh::kBN - 1) / Sh::kBN;
   p.m_tiles = (int)((p.n_rows + Sh::kBM - 1) / Sh::kBM);
@@ -679,8 +716,9 @@ int launch_linear_shape(LinearParams p, hipStream_t stream) {
     };
     return p.K % kStep != 0 ? launch(std::true_type{}) : launch(std::false_type{});
   } else {
-    if (!allow_full_lds<fp8_linear_kernel<Sh>>()) return -1;
-    return launch_kernel(fp8_linear_kernel<Sh>, dim3(tiles), dim3(Sh::kWaves * 64), (size_t)Sh::kSmem, stream, p);
+    if (!allow_full_lds<fp8_linear_kernel<Sh, G>>()) return -1;
+    return launch_kernel(fp8_linear_kernel<Sh, G>, dim3(tiles), dim3(Sh::kWaves * G * 64), (size_t)(G * Sh::kSmem),
+                         stream, p);
   }
 }
 
@@ -706,19 +744,33 @@ double shape_time(const ShapeTime& t, long long n_rows, int K, int F, int side, 
   return rounds > bytes ? rounds : bytes;
 }
 
-enum class LinearTile { kLarge, kMedium, kSmall, kRows };
+enum class LinearTile { kLarge, kMedium, kSmall, kShared, kRows };
 LinearTile choose_linear(long long n_rows, int K, int F) {
-  const double small = shape_time(kSmallTime, n_rows, K, F, 64, 512);
-  // A few rows: every workgroup of 16 features reads them and its part of the weight, at about 6 TB/s from the L2s (us,
-  // 64 x 64 tiles / this: 1 x 2048 -> 12288 9.5 / 6.6, 1 x 5504 -> 2048 19.6 / 5.7, 64 x 5504 -> 2048 19.9 / 16.2,
-  // 64 x 2048 -> 11008 9.8 / 19.2).
-  if (n_rows <= 64 && 2.0 + (double)(F / 16) * (double)(n_rows + 16) * K / 6e6 < small) return LinearTile::kRows;
+  double small = shape_time(kSmallTime, n_rows, K, F, 64, 512);
+  LinearTile of_64 = LinearTile::kSmall;
+  // groups that share the channels: one workgroup per CU, so for one round of tiles
+  const long long tiles = (n_rows + 63) / 64 * (F / 64);
+  if (tiles <= kCus) {
+    const int part = ((K + kStep - 1) / kStep + kShared - 1) / kShared;
+    const double shared = 4.15 + part * (0.66 + 0.4 / kCus * (double)tiles);
+    if (shared < small) {
+      small = shared;
+      of_64 = LinearTile::kShared;
+    }
+  }
+  // A few rows: every workgroup of 16 features reads them and its part of the weight, from the L2s (us, 64 x 64 tiles /
+  // this: 1 x 2048 -> 12288 8.5 / 7.1, 1 x 5504 -> 2048 11.6 / 6.1, 17 x 5504 -> 2048 11.8 / 8.9, 64 x 5504 -> 2048 13.3
+  // / 16.5, 17 x 2048 -> 11008 9.1 / 10.7, 64 x 768 -> 2304 5.5 / 4.7).
+  if (n_rows <= 64) {
+    const double filled = 0.15 + 0.026 * (F / 16), rate = filled < 6.2 ? filled : 6.2;       // TB/s
+    if (2.3 + (double)(F / 16) * (double)(n_rows + 16) * K / (1e6 * rate) < small) return LinearTile::kRows;
+  }
   const double medium = shape_time(kMediumTime, n_rows, K, F, 128, 512);
   // 256 x 256 tiles are moved back from the ends, and look a step ahead
   const double large = n_rows >= kLargeSide && F >= kLargeSide && K > kStep
                            ? shape_time(kLargeTime, n_rows, K, F, 256, (int)kCus) : 1e30;
   if (large <= medium && large <= small) return LinearTile::kLarge;
-  return small <= medium ? LinearTile::kSmall : LinearTile::kMedium;
+  return small <= medium ? of_64 : LinearTile::kMedium;
 }
 
 // Whether the XCDs take the token tiles of 256 rows in turn, or each a contiguous piece of all tiles.  In turn is the
@@ -734,6 +786,7 @@ int launch_linear(LinearParams p, hipStream_t stream) {
   switch (choose_linear(p.n_rows, p.K, p.F)) {
     case LinearTile::kRows: return launch_linear_rows(p, stream);
     case LinearTile::kSmall: return launch_linear_shape<LinearSmall>(p, stream);
+    case LinearTile::kShared: return launch_linear_shape<LinearShared, kShared>(p, stream);
     case LinearTile::kMedium: return launch_linear_shape<LinearMedium>(p, stream);
     default:
       p.interleave = interleave_large(p.n_rows, p.F);
@@ -803,8 +856,16 @@ extern "C" int aeris_linear_fp8_plan(int64_t n_rows, int32_t channels, int32_t o
   if (!tile || !in_turn) return AERIS_ERR_NULL_POINTER;
   if (const int rc = check_linear(n_rows, channels, out_features)) return rc;
   const LinearTile t = choose_linear(n_rows, channels, out_features);
-  *tile = t == LinearTile::kLarge ? 256 : t == LinearTile::kMedium ? 128 : t == LinearTile::kSmall ? 64 : 16;
+  *tile = t == LinearTile::kLarge ? 256 : t == LinearTile::kMedium ? 128 : t == LinearTile::kRows ? 16 : 64;
   *in_turn = t == LinearTile::kLarge && interleave_large(n_rows, out_features);
+  return AERIS_OK;
+}
+
+extern "C" int aeris_linear_fp8_parts(int64_t n_rows, int32_t channels, int32_t out_features, int32_t* parts) {
+  if (!parts) return AERIS_ERR_NULL_POINTER;
+  if (const int rc = check_linear(n_rows, channels, out_features)) return rc;
+  const LinearTile t = choose_linear(n_rows, channels, out_features);
+  *parts = t == LinearTile::kRows ? kRowsWaves : t == LinearTile::kShared ? kShared : 1;
   return AERIS_OK;
 }
 

@@ -148,3 +148,9 @@ def test_linear_bwd_refuses_and_sizes_its_workspace():
         assert call(**{name: None}) == -1 and call(**{name: ODD}) == -7
     assert call(dx=None, dw=None) == -1 and call(dx=ODD) == -7 and call(dw=ODD) == -7
     assert call(bytes=need - 1) == -8 and call(n=0) == -2 and call(c=96) == -3 and call(f=72) == -3
+
+
+def test_linear_tells_its_parts():
+    assert [B.aeris_linear_fp8_parts(*v) for v in ((1, 2048, 12288), (128, 5504, 2048), (172800, 2048, 11008))] == [8, 4, 1]
+    with pytest.raises(B.AerisError):
+        B.aeris_linear_fp8_parts(8, 96, 64)

@@ -572,3 +572,30 @@ def test_linear_refuses_operands_of_another_place():
     with pytest.raises(AssertionError):
         B.aeris_linear_fp8_bwd(w8, ws, w8, ws, torch.zeros(64, 64, dtype=torch.bfloat16, device="cuda"),
                                workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda")[::2])
+
+
+@pytest.mark.parametrize("n,c,f,parts", [
+    (64, 2048, 11008, 4), (65, 5504, 64, 4), (192, 2112, 128, 4), (129, 1088, 128, 4), (1000, 1216, 1024, 4), (65, 704, 64, 4),
+    (257, 448, 64, 4), (1000, 64, 2048, 1), (2500, 1600, 2112, 1), (1, 5504, 2048, 8), (17, 5504, 2048, 8), (64, 768, 2304, 8),
+])
+def test_linear_in_parts_of_the_channels(n, c, f, parts):
+    """Groups of waves that share the channels: parts of equal and unequal length, half a last block, ends of tiles."""
+    assert B.aeris_linear_fp8_parts(n, c, f) == parts
+    test_linear(n, c, f)
+
+
+def test_linear_keeps_scales_and_nan_in_parts_of_the_channels():
+    """Blocks of unlike scales in every part, whole numbers: exact.  A row that is not finite stays alone."""
+    n, c, f = 200, 1344, 128
+    assert B.aeris_linear_fp8_parts(n, c, f) == 4
+    rng = np.random.default_rng(3)
+    q = lambda rows: fo.encode(rng.integers(-8, 9, (rows, c)).astype(float))
+    scales = lambda rows: np.concatenate([rng.integers(124, 131, (rows, 11)), np.full((rows, 1), 127)], 1).astype(np.uint8)
+    xq, xs, wq, ws = q(n), scales(n), q(f), scales(f)
+    want = fo.dequantize(xq, xs) @ fo.dequantize(wq, ws).T               # multiples of 2^-6, below 2^18: exact
+    want = torch.from_numpy(want).float().bfloat16()
+    y = B.aeris_linear_fp8_fwd(*dev(xq, xs), *dev(wq, ws)).cpu()
+    assert torch.equal(y, want)
+    xq[150, c - 1] = 0x7f
+    y = B.aeris_linear_fp8_fwd(*dev(xq, xs), *dev(wq, ws)).cpu()
+    assert torch.isnan(y[150]).all() and torch.equal(y[:150], want[:150]) and torch.equal(y[151:], want[151:])
