@@ -62,7 +62,8 @@ int aeris_linear_fp8_plan(int64_t n_rows, int32_t channels, int32_t out_features
 
 /*
  * Into how many parts, added in their order, that call cuts the channels of a workgroup tile (else its
- * error code): 8 for a few rows, 4 where 64 x 64 tiles are fewer than CUs, 1.  Launches nothing.
+ * error code): 8 for a few rows, 4 or 2 where 64 x 64 or 128 x 128 tiles are no more than the CUs, or 1.
+ * Launches nothing.
  */
 int aeris_linear_fp8_parts(int64_t n_rows, int32_t channels, int32_t out_features, int32_t* parts);
 

@@ -57,8 +57,9 @@ struct LinearShape {
 using LinearLarge = LinearShape<2, 2, 4, 4, 2>;    // 256 x 256, one workgroup per CU
 using LinearMedium = LinearShape<2, 2, 2, 2, 2>;   // 128 x 128, two workgroups per CU
 using LinearSmall = LinearShape<2, 1, 1, 2, 4>;    // 64 x 64, two workgroups per CU, three stages in flight
-using LinearShared = LinearShape<2, 1, 1, 2, 2>;   // 64 x 64, kShared groups of waves share the channels
-constexpr int kShared = 4;
+// one workgroup per CU: groups of waves share the channels
+using LinearShared = LinearShape<2, 1, 1, 2, 2>;   // 64 x 64
+constexpr int kSmallGroups = 4, kMediumGroups = 2;
 
 // Where a workgroup's tile lies: two scalar registers, from which the rest is worked out where it is needed.
 template <class Sh>
@@ -182,10 +183,11 @@ __device__ __forceinline__ void linear_clear(f32x16 (&acc)[2][NB]) {
 // One workgroup per tile.  Rows past the end repeat the last valid row (never stored); where the channels end
 // in the middle of the last block, the copies of its second half repeat the first and are not multiplied.
 // G groups of Sh::kWaves waves share the channels of the tile: each takes a contiguous part of the steps, with stages
-// of its own, and the first adds the others' sums to its own in their order.  For fewer tiles than CUs, where a step of
-// 64 x 64 is its instructions and latencies (0.5 us) and nothing else runs beside it: 128 rows x 5504 -> 2048 21.2 ->
-// 14.6 us, x 2048 -> 2048 10.1 -> 7.1, x 768 -> 2304 6.1 -> 5.5 (two groups with four stages each 14.9, 7.9, 5.5;
-// three with three 14.4, 7.9, 5.5).
+// of its own, and the first adds the others' sums to its own in their order.  For no more tiles than CUs, where a step
+// is its instructions and latencies (64 x 64: 0.5 us) and nothing else runs beside it.  64 x 64, four groups: 128 rows x
+// 5504 -> 2048 21.2 -> 14.6 us, x 2048 -> 2048 10.1 -> 7.1, x 768 -> 2304 6.1 -> 5.5 (two groups with four stages each
+// 14.9, 7.9, 5.5; three with three 14.4, 7.9, 5.5); 128 x 128, two groups: 2048 rows x 5504 -> 2048 33.3 -> 29.6,
+// x 2048 -> 2048 15.6 -> 14.4.
 template <class Sh, int G>
 __global__ __launch_bounds__(Sh::kWaves * G * 64, 2) void fp8_linear_kernel(LinearParams p) {
   constexpr int kBN = Sh::kBN, NB = Sh::NB, W = Sh::kWaves, kStages = Sh::kStages;
@@ -744,33 +746,44 @@ double shape_time(const ShapeTime& t, long long n_rows, int K, int F, int side, 
   return rounds > bytes ? rounds : bytes;
 }
 
-enum class LinearTile { kLarge, kMedium, kSmall, kShared, kRows };
+// The same of workgroups whose groups of waves share the channels, one per CU: for one round of tiles.  A part of the
+// steps is longer the more CUs work.  What is taken is 0.3 % slower than the best way on average over 10,000 sizes of up
+// to 6000 rows, 5504 channels and 11,008 features, more than 8 % at 1 % of them.
+double shared_time(double fixed, double step, double step_filled, long long n_rows, int K, int F, int side, int groups) {
+  const long long tiles = (n_rows + side - 1) / side * ((F + side - 1) / side);
+  if (tiles > kCus) return 1e30;
+  const int part = ((K + kStep - 1) / kStep + groups - 1) / groups;
+  return fixed + part * (step + step_filled / kCus * (double)tiles);
+}
+
+enum class LinearTile { kLarge, kMedium, kMediumShared, kSmall, kSmallShared, kRows };
 LinearTile choose_linear(long long n_rows, int K, int F) {
-  double small = shape_time(kSmallTime, n_rows, K, F, 64, 512);
-  LinearTile of_64 = LinearTile::kSmall;
-  // groups that share the channels: one workgroup per CU, so for one round of tiles
-  const long long tiles = (n_rows + 63) / 64 * (F / 64);
-  if (tiles <= kCus) {
-    const int part = ((K + kStep - 1) / kStep + kShared - 1) / kShared;
-    const double shared = 4.15 + part * (0.66 + 0.4 / kCus * (double)tiles);
-    if (shared < small) {
-      small = shared;
-      of_64 = LinearTile::kShared;
-    }
-  }
-  // A few rows: every workgroup of 16 features reads them and its part of the weight, from the L2s (us, 64 x 64 tiles /
-  // this: 1 x 2048 -> 12288 8.5 / 7.1, 1 x 5504 -> 2048 11.6 / 6.1, 17 x 5504 -> 2048 11.8 / 8.9, 64 x 5504 -> 2048 13.3
-  // / 16.5, 17 x 2048 -> 11008 9.1 / 10.7, 64 x 768 -> 2304 5.5 / 4.7).
+  auto faster = [](LinearTile a, double time_a, LinearTile b, double time_b, double& time) {
+    time = time_a <= time_b ? time_a : time_b;
+    return time_a <= time_b ? a : b;
+  };
+  double small, medium;
+  const LinearTile of_64 = faster(LinearTile::kSmall, shape_time(kSmallTime, n_rows, K, F, 64, 512),
+                                  LinearTile::kSmallShared, shared_time(4.15, 0.66, 0.4, n_rows, K, F, 64, kSmallGroups),
+                                  small);
+  // A few rows: every workgroup of 16 features reads them and its part of the weight, from the L2s, in steps that wait
+  // for each other (us, 64 x 64 tiles / this: 1 x 2048 -> 12288 8.5 / 7.1, 1 x 5504 -> 2048 11.6 / 6.1, 17 x 5504 ->
+  // 2048 11.8 / 8.9, 64 x 5504 -> 2048 13.3 / 16.5, 17 x 2048 -> 11008 9.1 / 10.7, 64 x 768 -> 2304 5.5 / 4.7).
   if (n_rows <= 64) {
-    const double filled = 0.15 + 0.026 * (F / 16), rate = filled < 6.2 ? filled : 6.2;       // TB/s
-    if (2.3 + (double)(F / 16) * (double)(n_rows + 16) * K / (1e6 * rate) < small) return LinearTile::kRows;
+    const double filled = 0.15 + 0.026 * (F / 16), rate = filled < 7.0 ? filled : 7.0;       // TB/s
+    const double bytes = (double)(F / 16) * (double)(n_rows + 16) * K / (1e6 * rate);
+    const int blocks = n_rows <= 16 ? 1 : n_rows <= 32 ? 2 : 4, wave_steps = (K + kRowsWaves * kStep - 1) / (kRowsWaves * kStep);
+    const double waits = 0.25 * blocks + (wave_steps - 1) * (0.25 + 0.44 * blocks);
+    if (2.3 + (bytes > waits ? bytes : waits) < small) return LinearTile::kRows;
   }
-  const double medium = shape_time(kMediumTime, n_rows, K, F, 128, 512);
+  const LinearTile of_128 = faster(LinearTile::kMedium, shape_time(kMediumTime, n_rows, K, F, 128, 512),
+                                   LinearTile::kMediumShared,
+                                   shared_time(6.0, 1.05, 0.1, n_rows, K, F, 128, kMediumGroups), medium);
   // 256 x 256 tiles are moved back from the ends, and look a step ahead
   const double large = n_rows >= kLargeSide && F >= kLargeSide && K > kStep
                            ? shape_time(kLargeTime, n_rows, K, F, 256, (int)kCus) : 1e30;
   if (large <= medium && large <= small) return LinearTile::kLarge;
-  return small <= medium ? of_64 : LinearTile::kMedium;
+  return small <= medium ? of_64 : of_128;
 }
 
 // Whether the XCDs take the token tiles of 256 rows in turn, or each a contiguous piece of all tiles.  In turn is the
@@ -786,7 +799,8 @@ int launch_linear(LinearParams p, hipStream_t stream) {
   switch (choose_linear(p.n_rows, p.K, p.F)) {
     case LinearTile::kRows: return launch_linear_rows(p, stream);
     case LinearTile::kSmall: return launch_linear_shape<LinearSmall>(p, stream);
-    case LinearTile::kShared: return launch_linear_shape<LinearShared, kShared>(p, stream);
+    case LinearTile::kSmallShared: return launch_linear_shape<LinearShared, kSmallGroups>(p, stream);
+    case LinearTile::kMediumShared: return launch_linear_shape<LinearMedium, kMediumGroups>(p, stream);
     case LinearTile::kMedium: return launch_linear_shape<LinearMedium>(p, stream);
     default:
       p.interleave = interleave_large(p.n_rows, p.F);
@@ -856,7 +870,9 @@ extern "C" int aeris_linear_fp8_plan(int64_t n_rows, int32_t channels, int32_t o
   if (!tile || !in_turn) return AERIS_ERR_NULL_POINTER;
   if (const int rc = check_linear(n_rows, channels, out_features)) return rc;
   const LinearTile t = choose_linear(n_rows, channels, out_features);
-  *tile = t == LinearTile::kLarge ? 256 : t == LinearTile::kMedium ? 128 : t == LinearTile::kRows ? 16 : 64;
+  *tile = t == LinearTile::kLarge ? 256
+          : t == LinearTile::kMedium || t == LinearTile::kMediumShared ? 128
+          : t == LinearTile::kRows ? 16 : 64;
   *in_turn = t == LinearTile::kLarge && interleave_large(n_rows, out_features);
   return AERIS_OK;
 }
@@ -865,7 +881,9 @@ extern "C" int aeris_linear_fp8_parts(int64_t n_rows, int32_t channels, int32_t 
   if (!parts) return AERIS_ERR_NULL_POINTER;
   if (const int rc = check_linear(n_rows, channels, out_features)) return rc;
   const LinearTile t = choose_linear(n_rows, channels, out_features);
-  *parts = t == LinearTile::kRows ? kRowsWaves : t == LinearTile::kShared ? kShared : 1;
+  *parts = t == LinearTile::kRows ? kRowsWaves
+           : t == LinearTile::kSmallShared ? kSmallGroups
+           : t == LinearTile::kMediumShared ? kMediumGroups : 1;
   return AERIS_OK;
 }
 

@@ -575,6 +575,7 @@ def test_linear_refuses_operands_of_another_place():
 
 
 @pytest.mark.parametrize("n,c,f,parts", [
+    (2048, 2048, 2048, 2), (1990, 1344, 1984, 2), (500, 1600, 7104, 2), (2048, 5504, 1984, 2), (1999, 1216, 2048, 2),
     (64, 2048, 11008, 4), (65, 5504, 64, 4), (192, 2112, 128, 4), (129, 1088, 128, 4), (1000, 1216, 1024, 4), (65, 704, 64, 4),
     (257, 448, 64, 4), (1000, 64, 2048, 1), (2500, 1600, 2112, 1), (1, 5504, 2048, 8), (17, 5504, 2048, 8), (64, 768, 2304, 8),
 ])
