@@ -906,17 +906,24 @@ def aeris_linear_fp8_bwd(x8, xs, wt8, wts, dy, want_dx=True, want_dweight=True, 
         c = cx
     if not (want_dx or want_dweight):
         raise ValueError("aeris_linear_fp8_bwd: neither dx nor dweight is wanted")
-    if want_dx and dx is None:
-        dx = torch.empty((n, c), dtype=torch.bfloat16, device=dy.device)
-    if want_dweight and dweight is None:
-        dweight = torch.empty((f, c), dtype=torch.float32, device=dy.device)
-    assert not want_dx or _rows(dx) == (n, c)
-    assert not want_dweight or (dweight.shape == (f, c) and dweight.is_contiguous() and dweight.dtype == torch.float32)
+    if want_dx:
+        if dx is None:
+            dx = dy.new_empty((n, c))
+        else:
+            assert _rows(dx) == (n, c)
+    if want_dweight:
+        if dweight is None:
+            dweight = dy.new_empty((f, c), dtype=torch.float32)
+        else:
+            assert dweight.shape == (f, c) and dweight.is_contiguous() and dweight.dtype == torch.float32
     if workspace is None:
-        workspace = torch.empty(max(aeris_linear_fp8_bwd_workspace_bytes(n, c, f), 16), dtype=torch.uint8,
-                                device=dy.device)
+        workspace = dy.new_empty(max(aeris_linear_fp8_bwd_workspace_bytes(n, c, f), 16), dtype=torch.uint8)
     assert workspace.is_contiguous()
-    _here(dy, dx, dweight, workspace, *((wt8, wts) if want_dx else ()), *((x8, xs) if want_dweight else ()))
+    _here(dy, workspace)
+    if want_dx:
+        _here(dx, wt8, wts)
+    if want_dweight:
+        _here(dweight, x8, xs)
     rc = load().aeris_linear_fp8_bwd(_ptr(x8) if want_dweight else None, _ptr(xs) if want_dweight else None,
                                      _ptr(wt8) if want_dx else None, _ptr(wts) if want_dx else None,
                                      dy.data_ptr(), n, c, f, dx.data_ptr() if want_dx else None,

@@ -818,28 +818,26 @@ int check_linear(int64_t n_rows, int32_t channels, int32_t features) {
 bool bad16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) != 0; }
 size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// The workspace of the gradients: dy quantised for dx; then, in the same place, x in bf16 for dW and what
-// the product of dW needs.
+// The workspace of the gradients: x in bf16 and, behind it, what the product of dW needs; dy quantised for the product
+// of dx, which comes first, in the place of the latter where that is large enough, else of all of it.
 struct Backward {
-  size_t dys;             // offset of dy's scales
   size_t wgrad;           // offset of the workspace of the product of dW
+  size_t dy, dys;         // offsets of dy's values and scales
   size_t bytes;
 };
-Backward backward_layout(int64_t n_rows, int32_t channels, int32_t features) {
-  Backward b;
-  b.dys = round256((size_t)n_rows * features);
-  b.wgrad = round256((size_t)n_rows * channels * 2);
-  const size_t for_dx = b.dys + round256((size_t)n_rows * scale_pitch(features));
-  const size_t for_dw = b.wgrad + aeris_linear_bwd_workspace_bytes(n_rows, channels, features);
-  b.bytes = for_dx > for_dw ? for_dx : for_dw;
-  return b;
-}
-
-// The limits of both products of the backward pass.
-int check_linear_bwd(int64_t n_rows, int32_t channels, int32_t features) {
+// AERIS_OK if both products of the backward pass accept the size, else an AERIS_ERR_ code.
+int backward_layout(int64_t n_rows, int32_t channels, int32_t features, Backward& b) {
   if (const int rc = check_linear(n_rows, features, channels)) return rc;
   if ((long long)channels * features >= (1LL << 31)) return AERIS_ERR_INVALID_SHAPE;
-  return aeris_linear_bwd_workspace_bytes(n_rows, channels, features) == 0 ? AERIS_ERR_INVALID_SHAPE : AERIS_OK;
+  const size_t for_dw = aeris_linear_bwd_workspace_bytes(n_rows, channels, features);
+  if (for_dw == 0) return AERIS_ERR_INVALID_SHAPE;
+  b.wgrad = round256((size_t)n_rows * channels * 2);
+  const size_t values = round256((size_t)n_rows * features);
+  const size_t for_dx = values + round256((size_t)n_rows * scale_pitch(features));
+  b.dy = for_dx <= for_dw ? b.wgrad : 0;
+  b.dys = b.dy + values;
+  b.bytes = b.wgrad + for_dw > for_dx ? b.wgrad + for_dw : for_dx;
+  return AERIS_OK;
 }
 
 }  // namespace
@@ -888,8 +886,8 @@ extern "C" int aeris_linear_fp8_parts(int64_t n_rows, int32_t channels, int32_t 
 }
 
 extern "C" size_t aeris_linear_fp8_bwd_workspace_bytes(int64_t n_rows, int32_t channels, int32_t out_features) {
-  if (check_linear_bwd(n_rows, channels, out_features) != AERIS_OK) return 0;
-  return backward_layout(n_rows, channels, out_features).bytes;
+  Backward at;
+  return backward_layout(n_rows, channels, out_features, at) == AERIS_OK ? at.bytes : 0;
 }
 
 extern "C" int aeris_linear_fp8_bwd(const void* x8, const void* xs, const void* wt8, const void* wts, const void* dy,
@@ -897,26 +895,31 @@ extern "C" int aeris_linear_fp8_bwd(const void* x8, const void* xs, const void* 
                                     void* workspace, size_t workspace_bytes, void* hip_stream) {
   if (!dy || !workspace || (!dx && !dweight) || (dx && (!wt8 || !wts)) || (dweight && (!x8 || !xs)))
     return AERIS_ERR_NULL_POINTER;
-  if (const int rc = check_linear_bwd(n_rows, channels, out_features)) return rc;
+  Backward at;
+  if (const int rc = backward_layout(n_rows, channels, out_features, at)) return rc;
   if (bad16(x8) || bad16(xs) || bad16(wt8) || bad16(wts) || bad16(dy) || bad16(dx) || bad16(dweight) ||
       bad16(workspace))
     return AERIS_ERR_MISALIGNED;
-  const Backward at = backward_layout(n_rows, channels, out_features);
   if (workspace_bytes < at.bytes) return AERIS_ERR_WORKSPACE_TOO_SMALL;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   unsigned char* space = static_cast<unsigned char*>(workspace);
+  const unsigned char *q = static_cast<const unsigned char*>(x8), *qs = static_cast<const unsigned char*>(xs);
+  bf16_t* const x = reinterpret_cast<bf16_t*>(space);
+  // one launch for the operands of both products where they do not share memory: 2 us less on the host
+  const bool together = dx && dweight && at.dy != 0;
+  if (together && launch_fp8_backward_operands(static_cast<const bf16_t*>(dy), out_features, space + at.dy,
+                                               space + at.dys, q, qs, channels, x, n_rows, st) != 0)
+    return AERIS_ERR_HIP_LAUNCH;
   if (dx) {
-    if (launch_fp8_quantize_rows(dy, false, n_rows, out_features, space, space + at.dys, st) != 0)
+    if (!together && launch_fp8_quantize_rows(dy, false, n_rows, out_features, space + at.dy, space + at.dys, st) != 0)
       return AERIS_ERR_HIP_LAUNCH;
-    if (const int rc = aeris_linear_fp8_fwd(space, space + at.dys, wt8, wts, n_rows, out_features, channels, dx,
+    if (const int rc = aeris_linear_fp8_fwd(space + at.dy, space + at.dys, wt8, wts, n_rows, out_features, channels, dx,
                                             hip_stream))
       return rc;
   }
   if (dweight) {
-    if (launch_fp8_dequantize(static_cast<const unsigned char*>(x8), static_cast<const unsigned char*>(xs), n_rows,
-                              channels, reinterpret_cast<bf16_t*>(space), st) != 0)
-      return AERIS_ERR_HIP_LAUNCH;
-    return aeris_linear_bwd(space, nullptr, dy, n_rows, channels, out_features, nullptr, dweight, space + at.wgrad,
+    if (!together && launch_fp8_dequantize(q, qs, n_rows, channels, x, st) != 0) return AERIS_ERR_HIP_LAUNCH;
+    return aeris_linear_bwd(x, nullptr, dy, n_rows, channels, out_features, nullptr, dweight, space + at.wgrad,
                             workspace_bytes - at.wgrad, hip_stream);
   }
   return AERIS_OK;

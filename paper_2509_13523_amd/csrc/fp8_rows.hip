@@ -21,16 +21,16 @@ constexpr int kThreads256 = 256;
 constexpr int kGroups = kThreads256 / kBlockLanes;   // blocks a workgroup works on side by side
 constexpr unsigned kMostBlocks = 1u << 22;           // workgroups of a launch over blocks
 
-// Blocks a workgroup's 16 groups of lanes walk over: all blocks of the rows [r0, r1), 16 apart.
+// Blocks the 16 groups of lanes of workgroup `index` of `count` walk over: all blocks of its rows, 16 apart.
 struct BlockWalk {
   long long row, end;
   int block, blocks;
   int row_step, block_step;
-  __device__ __forceinline__ void init(long long n_rows, int cols) {
+  __device__ __forceinline__ void init(long long n_rows, int cols, unsigned index, unsigned count) {
     blocks = (cols + AERIS_FP8_BLOCK - 1) / AERIS_FP8_BLOCK;
     const int group = threadIdx.x / kBlockLanes;
-    const long long r0 = n_rows * blockIdx.x / gridDim.x;
-    end = n_rows * (blockIdx.x + 1) / gridDim.x;
+    const long long r0 = n_rows * index / count;
+    end = n_rows * (index + 1) / count;
     row = r0 + group / blocks;
     block = group % blocks;
     row_step = kGroups / blocks;
@@ -57,12 +57,12 @@ unsigned walk_grid(long long n_rows, int cols, int each) {
 
 // ---- rows of bf16 or fp32, by rows -----------------------------------------------------------------
 template <typename T>
-__global__ __launch_bounds__(kThreads256) void fp8_quantize_rows_kernel(const T* __restrict__ x, long long n_rows,
-                                                                        int cols, unsigned char* __restrict__ x8,
-                                                                        unsigned char* __restrict__ xs) {
+__device__ __forceinline__ void quantize_rows(const T* __restrict__ x, long long n_rows, int cols,
+                                              unsigned char* __restrict__ x8, unsigned char* __restrict__ xs,
+                                              unsigned index, unsigned count) {
   const int lane = threadIdx.x & (kBlockLanes - 1), pitch = scale_pitch(cols);
   BlockWalk at;
-  at.init(n_rows, cols);
+  at.init(n_rows, cols, index, count);
   // every lane of a wave takes part in the rotations, so all leave together
   for (; __any(at.valid()); at.step()) {
     const int c = at.block * AERIS_FP8_BLOCK + lane * 8;
@@ -78,6 +78,12 @@ __global__ __launch_bounds__(kThreads256) void fp8_quantize_rows_kernel(const T*
     if (in) *reinterpret_cast<u32x2*>(x8 + at.row * cols + c) = q;
     if (at.valid()) store_scale(xs + at.row * pitch, at.block, at.blocks, pitch, byte, lane);
   }
+}
+template <typename T>
+__global__ __launch_bounds__(kThreads256) void fp8_quantize_rows_kernel(const T* __restrict__ x, long long n_rows,
+                                                                        int cols, unsigned char* __restrict__ x8,
+                                                                        unsigned char* __restrict__ xs) {
+  quantize_rows(x, n_rows, cols, x8, xs, blockIdx.x, gridDim.x);
 }
 
 // ---- the transpose, and by rows from the same read ---------------------------------------------------
@@ -269,13 +275,12 @@ __global__ __launch_bounds__(kThreads256) void fp8_quantize_transposed_kernel(
 }
 
 // ---- back to bf16, exact ---------------------------------------------------------------------------
-__global__ __launch_bounds__(kThreads256) void fp8_dequantize_kernel(const unsigned char* __restrict__ x8,
-                                                                     const unsigned char* __restrict__ xs,
-                                                                     long long n_rows, int cols,
-                                                                     bf16_t* __restrict__ x) {
+__device__ __forceinline__ void dequantize_rows(const unsigned char* __restrict__ x8, const unsigned char* __restrict__ xs,
+                                                long long n_rows, int cols, bf16_t* __restrict__ x, unsigned index,
+                                                unsigned count) {
   const int lane = threadIdx.x & (kBlockLanes - 1), pitch = scale_pitch(cols);
   BlockWalk at;
-  at.init(n_rows, cols);
+  at.init(n_rows, cols, index, count);
   for (; at.valid(); at.step()) {
     const int c = at.block * AERIS_FP8_BLOCK + lane * 8;
     if (c >= cols) continue;
@@ -291,6 +296,22 @@ __global__ __launch_bounds__(kThreads256) void fp8_dequantize_kernel(const unsig
     }
     *reinterpret_cast<u32x4*>(x + at.row * cols + c) = o;
   }
+}
+__global__ __launch_bounds__(kThreads256) void fp8_dequantize_kernel(const unsigned char* __restrict__ x8,
+                                                                     const unsigned char* __restrict__ xs,
+                                                                     long long n_rows, int cols,
+                                                                     bf16_t* __restrict__ x) {
+  dequantize_rows(x8, xs, n_rows, cols, x, blockIdx.x, gridDim.x);
+}
+
+// What both gradients of a projection need, dy quantised (the first `first` workgroups) and x in bf16 (the others),
+// side by side in one launch.
+__global__ __launch_bounds__(kThreads256) void fp8_backward_operands_kernel(
+    const bf16_t* __restrict__ dy, int features, unsigned char* __restrict__ dy8, unsigned char* __restrict__ dys,
+    unsigned first, const unsigned char* __restrict__ x8, const unsigned char* __restrict__ xs, int channels,
+    bf16_t* __restrict__ x, long long n_rows) {
+  if (blockIdx.x < first) quantize_rows(dy, n_rows, features, dy8, dys, blockIdx.x, first);
+  else dequantize_rows(x8, xs, n_rows, channels, x, blockIdx.x - first, gridDim.x - first);
 }
 
 // ---- gated residual + RMSNorm + modulation --------------------------------------------------------------
@@ -424,7 +445,7 @@ __global__ __launch_bounds__(kThreads256) void swiglu_fp8_kernel(const bf16_t* _
                                                                  unsigned char* __restrict__ gs) {
   const int lane = threadIdx.x & (kBlockLanes - 1), pitch = scale_pitch(hidden);
   BlockWalk at;
-  at.init(n_rows, hidden);
+  at.init(n_rows, hidden, blockIdx.x, gridDim.x);
   constexpr int U = kGateAhead;
   while (__any(at.valid())) {
     u32x4 u[U], v[U];
@@ -508,6 +529,14 @@ int launch_fp8_dequantize(const unsigned char* x8, const unsigned char* xs, long
                           hipStream_t stream) {
   return launch_kernel(fp8_dequantize_kernel, dim3(walk_grid(n_rows, cols, 4)), dim3(kThreads256), 0, stream, x8, xs,
                        n_rows, cols, x);
+}
+
+int launch_fp8_backward_operands(const bf16_t* dy, int features, unsigned char* dy8, unsigned char* dys,
+                                 const unsigned char* x8, const unsigned char* xs, int channels, bf16_t* x,
+                                 long long n_rows, hipStream_t stream) {
+  const unsigned first = walk_grid(n_rows, features, 4);
+  return launch_kernel(fp8_backward_operands_kernel, dim3(first + walk_grid(n_rows, channels, 4)), dim3(kThreads256), 0,
+                       stream, dy, features, dy8, dys, first, x8, xs, channels, x, n_rows);
 }
 
 }  // namespace aeris

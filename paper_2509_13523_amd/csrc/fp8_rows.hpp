@@ -14,5 +14,9 @@ int launch_fp8_quantize_rows(const void* x, bool f32, long long n_rows, int cols
                              unsigned char* xs, hipStream_t stream);
 int launch_fp8_dequantize(const unsigned char* x8, const unsigned char* xs, long long n_rows, int cols, bf16_t* x,
                           hipStream_t stream);
+// The first of dy [n_rows, features] and the second of x [n_rows, channels] in one launch.
+int launch_fp8_backward_operands(const bf16_t* dy, int features, unsigned char* dy8, unsigned char* dys,
+                                 const unsigned char* x8, const unsigned char* xs, int channels, bf16_t* x,
+                                 long long n_rows, hipStream_t stream);
 
 }  // namespace aeris
