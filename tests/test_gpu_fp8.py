@@ -600,3 +600,46 @@ def test_linear_keeps_scales_and_nan_in_parts_of_the_channels():
     xq[150, c - 1] = 0x7f
     y = B.aeris_linear_fp8_fwd(*dev(xq, xs), *dev(wq, ws)).cpu()
     assert torch.isnan(y[150]).all() and torch.equal(y[:150], want[:150]) and torch.equal(y[151:], want[151:])
+
+
+@pytest.mark.parametrize("power", [-126, -132, -140])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_quantize_rows_of_subnormal_numbers(power, dtype):
+    """Blocks below the smallest normal number: the smallest scale, codes down to zero, their signs kept."""
+    rng = np.random.default_rng(-power)
+    t, x = (bf16 if dtype == "bf16" else f32)(np.ldexp(rng.standard_normal((64, 192)), power))
+    x8, xs, xt8, xts = B.aeris_fp8_quantize(t, transposed=True)
+    torch.cuda.synchronize()
+    for got, want in ((codes(x8, xs), fo.quantize(x)), (codes(xt8, xts), fo.quantize(x.T))):
+        same_codes(got[0], want[0])
+        assert (got[1] == want[1]).all()
+
+
+def test_captured_gradients_and_products_of_few_tiles():
+    """Calls whose waves share the channels and both layouts of the gradients' workspace, captured and replayed with new
+    inputs in place, eager work between the replays."""
+    sizes = [(130, 1088, 192), (2100, 64, 128), (17, 2112, 64)]
+    ins, graph, outs = [], torch.cuda.CUDAGraph(), []
+    gen = torch.Generator(device="cuda").manual_seed(9)
+    draw = lambda *shape: torch.randn(*shape, device="cuda", generator=gen).bfloat16()
+    def call(x, w, dy):
+        x8, xs, _, _ = B.aeris_fp8_quantize(x)
+        w8, ws, wt8, wts = B.aeris_fp8_quantize(w, transposed=True)
+        return (B.aeris_linear_fp8_fwd(x8, xs, w8, ws),) + B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, dy)
+    for n, c, f in sizes:
+        ins.append((draw(n, c), draw(f, c), draw(n, f)))
+    for v in ins:
+        call(*v)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        outs = [call(*v) for v in ins]
+    for _ in range(3):
+        for v in ins:
+            for t in v:
+                t.copy_(draw(*t.shape))
+        want = [call(*v) for v in ins]
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, want):
+            assert all(same_bits(p, q) for p, q in zip(a, b))
+        draw(1000, 1000).float().sum().item()
