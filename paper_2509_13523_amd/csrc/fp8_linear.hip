@@ -120,7 +120,7 @@ __device__ __forceinline__ unsigned long long uniform(const void* ptr) {
          (uint32_t)__builtin_amdgcn_readfirstlane((int)a);
 }
 
-// The same with a constant distance behind the addresses, which goes into the instructions.
+// read_pair() with a constant distance behind the addresses, which goes into the instructions.
 __device__ __forceinline__ i32x8 read_tile(uint32_t lo, uint32_t hi, int behind) {
   const i32x4 a = *reinterpret_cast<const AERIS_LDS i32x4*>(reinterpret_cast<const AERIS_LDS char*>(lo) + behind);
   const i32x4 b = *reinterpret_cast<const AERIS_LDS i32x4*>(reinterpret_cast<const AERIS_LDS char*>(hi) + behind);
@@ -182,6 +182,9 @@ __device__ __forceinline__ void linear_clear(f32x16 (&acc)[2][NB]) {
 
 // One workgroup per tile.  Rows past the end repeat the last valid row (never stored); where the channels end
 // in the middle of the last block, the copies of its second half repeat the first and are not multiplied.
+// Bound by the LDS for long sums (a wave's 64 x 64 results need 127 of the 128 bytes a cycle that it gives), by the
+// latency of the first and last steps for short ones.  128 x 128 / 64 x 64 tiles, us: 172,800 x 2048 -> 11008 4030 / 8140,
+// 4096 x 2048 -> 2048 21 / 39, 1024 x 768 -> 2304 7.2 / 10.2, 512 x 768 -> 2304 6.9 / 6.8.
 // G groups of Sh::kWaves waves share the channels of the tile: each takes a contiguous part of the steps, with stages
 // of its own, and the first adds the others' sums to its own in their order.  For no more tiles than CUs, where a step
 // is its instructions and latencies (64 x 64: 0.5 us) and nothing else runs beside it.  64 x 64, four groups: 128 rows x
