@@ -437,6 +437,22 @@ __global__ __launch_bounds__(kThreads256) void residual_norm_fp8_kernel(NormPara
 }
 
 // ---- SwiGLU gate ------------------------------------------------------------------------------------
+// u sigma(u) v = u v / (1 + e^-u), whose e^-u passes fp32 below u = -88.7 and whose reciprocal the hardware takes for
+// zero from -87.4 on.  g is a number that a block can hold far beyond: down to u = -190 if v is large.
+constexpr float kGateFar = -87.f;
+// Below kGateFar: 1 + e^u is 1 in fp32, so g = u e^u v, with e^u = 2^(n + f), |f| <= 1/2, and 2^n applied in two parts,
+// of which the first goes to v: neither passes the range where g does not.  u log2 e in two parts too: rounded to 24 bits
+// it would carry 5e-6 into g.
+__device__ __forceinline__ float gate_far(float u, float v) {
+  constexpr float kLog2eRest = 1.9259629911e-8f;       // log2 e - kLog2e
+  const float held = u > -400.f ? u : -400.f;          // g is zero from -300 on
+  const float t = held * kLog2e, n = __builtin_rintf(t);
+  const float rest = __builtin_fmaf(held, kLog2eRest, __builtin_fmaf(held, kLog2e, -t));
+  const int e = (int)n, half = e >> 1;
+  const float factor = __builtin_fmaf(0.f, u, held);   // held, but NaN where u is infinite, as nearer to zero
+  return __builtin_ldexpf(__builtin_ldexpf(v, half) * (factor * __builtin_amdgcn_exp2f((t - n) + rest)), e - half);
+}
+
 // Two blocks per group of lanes, read before either is worked on, and no more per workgroup: 172,800 rows x 5504 832 us,
 // 5.7 TB/s (one block at a time in 8192 workgroups 991; results that pass the caches like the rest 981).
 constexpr int kGateAhead = 2;
@@ -474,6 +490,14 @@ __global__ __launch_bounds__(kThreads256) void swiglu_fp8_kernel(const bf16_t* _
 #pragma unroll
       for (int e = 0; e < 8; ++e)
         o[e] = uf[e] * __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(-uf[e] * kLog2e)) * vf[e];
+      // the most negative u has the largest bits
+      uint32_t lowest = 0;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) lowest = __float_as_uint(uf[e]) > lowest ? __float_as_uint(uf[e]) : lowest;
+      if (__builtin_expect(__any(lowest > __float_as_uint(kGateFar)), 0)) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) o[e] = uf[e] < kGateFar ? gate_far(uf[e], vf[e]) : o[e];
+      }
       u32x2 q;
       const uint32_t byte = quantize_block(o, q);
       if (in) __builtin_nontemporal_store(q, reinterpret_cast<u32x2*>(g8 + row[i] * hidden + c));

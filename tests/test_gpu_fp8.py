@@ -643,3 +643,43 @@ def test_captured_gradients_and_products_of_few_tiles():
         for a, b in zip(outs, want):
             assert all(same_bits(p, q) for p, q in zip(a, b))
         draw(1000, 1000).float().sum().item()
+
+
+@pytest.mark.parametrize("n,hidden,v_power", [(41, 64, 0), (41, 192, 20), (130, 576, 90), (130, 576, 125)])
+def test_swiglu_far_below_zero(n, hidden, v_power):
+    """Blocks of nothing but u < -80, where silu(u) v is held as long as the format holds it: 1 + exp(-u) passes fp32
+    below -88.7 and silu(u) leaves the normal numbers below -92, their product with a large v not before -180."""
+    rng = np.random.default_rng(n + hidden + v_power)
+    u = -80.0 - (12.0 + 0.8 * v_power) * rng.random((n, 1)) - rng.random((n, hidden))
+    v = rng.standard_normal((n, hidden)) * 2.0 ** v_power
+    u[0], u[1], u[2] = -87.0, -87.5, -3e38                # the border of the two ways, and a gate of zero
+    t, uv = bf16(np.concatenate([u, v], 1))
+    q, scales = codes(*B.aeris_swiglu_fp8_fwd(t))
+    g = bo.swiglu_fwd(uv)
+    assert (np.abs(g).max(1) > 2.0 ** -126).sum() > 3
+    # below the normal numbers fp32 has multiples of 2^-149, to half of which g is rounded: 1.07 * SLACK * 2^-131 covers it
+    close_quantized("g far", (q, scales), g, np.abs(g) + 2.0 ** -131)
+
+
+def test_swiglu_far_beside_near():
+    """Far values beside ordinary ones change nothing of those, and values that are not finite stay alone."""
+    rng = np.random.default_rng(53)
+    n, hidden = 24, 320
+    u, v = rng.standard_normal((2, n, hidden))
+    t, _ = bf16(np.concatenate([u, v], 1))
+    near = codes(*B.aeris_swiglu_fp8_fwd(t))
+    u[:, 9::16] = -90.0 - 50.0 * rng.random((n, hidden // 16))
+    u[5, 9], u[6, 9], u[7, 9] = -np.inf, np.inf, np.nan
+    t, uv = bf16(np.concatenate([u, v], 1))
+    q, scales = codes(*B.aeris_swiglu_fp8_fwd(t))
+    with np.errstate(invalid="ignore"):
+        g = bo.swiglu_fwd(uv)
+    lost = np.zeros((n, hidden), dtype=bool)
+    lost[5:8, 9] = True
+    assert ((q & 127) == 127)[lost].all() and not ((q & 127) == 127)[~lost].any()
+    g[lost], q[lost] = 0.0, 0
+    close_quantized("g mixed", (q, scales), g, np.abs(g))
+    ordinary = np.ones(hidden, dtype=bool)
+    ordinary[9::16] = False
+    same = np.repeat(scales[:, :3] == near[1][:, :3], 128, 1)[:, :hidden] & ordinary     # blocks of the same scale
+    assert same.sum() > n * hidden // 2 and (q[same] == near[0][same]).all()
