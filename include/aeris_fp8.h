@@ -94,9 +94,12 @@ int aeris_swiglu_fp8_fwd(const void* uv, int64_t n_rows, int32_t hidden, void* g
  * than 2^25 tiles of 64 x 64 in y.
  * Products of blocks accumulate in fp32 over the channels.  Inside the matrix instruction eight
  * neighbouring products are added before they join the accumulator, and what is below 2^-13 of the
- * largest of the eight is dropped: |error| <= 7 * 2^-13 * (sum over groups of eight channels of the
- * largest |x w| of the group), about 1e-5 of the result for operands of like size (bf16 results are
- * rounded by up to 2^-8 = 4e-3).
+ * largest of the eight is dropped; 16 channels at a time join it, which costs up to its last bit:
+ *     |error| <= 7 * 2^-13 * (sum over groups of eight channels of the largest |x w| of the group)
+ *                + (channels / 16 + 8) * 2^-23 * (sum over channels of |x w|),
+ * and y is rounded to bf16 (up to 2^-8 = 4e-3 of it).  For operands of like size that is about 1e-5 of
+ * the result for up to a few thousand channels; with the most channels and one large block among them
+ * the second term comes to 5e-4 of the sum of magnitudes, of which 2e-4 has been seen.
  */
 int aeris_linear_fp8_fwd(const void* x8, const void* xs, const void* w8, const void* ws,
                          int64_t n_rows, int32_t channels, int32_t out_features, void* y,

@@ -683,3 +683,46 @@ def test_swiglu_far_beside_near():
     ordinary[9::16] = False
     same = np.repeat(scales[:, :3] == near[1][:, :3], 128, 1)[:, :hidden] & ordinary     # blocks of the same scale
     assert same.sum() > n * hidden // 2 and (q[same] == near[0][same]).all()
+
+
+# --------------------------------------------------------------------------- sums over many channels
+MANY_CHANNELS = [(15, 65536, 64, 16, 8), (40, 65472, 64, 64, 4), (1000, 65536, 2048, 64, 1), (2500, 65472, 512, 64, 1),
+                 (700, 65536, 2048, 128, 2), (1500, 65472, 1024, 128, 2), (2500, 65472, 2048, 128, 1),
+                 (2500, 65536, 4096, 256, 1), (2500, 65472, 4096, 256, 1)]
+
+
+@pytest.mark.parametrize("n,c,f,tile,parts", MANY_CHANNELS)
+def test_sums_of_many_channels_beside_a_large_block(n, c, f, tile, parts):
+    """A first block that sums to one, thousands of products below its last bit, a last block that takes the one away
+    again; so in every part of the channels.  What is left shows each error of the sums, of which the header states
+        7 * 2^-13 * sum over groups of eight channels of the largest |x w|  +  (channels / 16 + 8) * 2^-23 * sum |x w|.
+    With one part the first term covers half of the errors here: each block brings only its largest product into it,
+    while each 16 channels lose up to a last bit of the one."""
+    assert B.aeris_linear_fp8_plan(n, c, f)[0] == tile and B.aeris_linear_fp8_parts(n, c, f) == parts
+    kinds, steps = 15, -(-c // 128)
+    x = np.outer(np.arange(1, kinds + 1) * 2.0 ** -30, np.ones(c))
+    for part in range(parts):
+        first, last = steps * part // parts, steps * (part + 1) // parts - 1
+        x[:, first * 128:first * 128 + 128] = 2.0 ** -7
+        x[:, last * 128:last * 128 + 128] = -1.0 / (min(c, last * 128 + 128) - last * 128)
+    xq, xs = fo.quantize(x)
+    assert (fo.dequantize(xq, xs) == x).all()
+    kind = torch.arange(n, device="cuda") % kinds
+    tile_rows = lambda a: torch.from_numpy(a).cuda()[kind]
+    w8, ws = fo.quantize(np.ones((1, c)))
+    repeat = lambda a: torch.from_numpy(a).cuda().expand(f, -1).contiguous()
+    y = B.aeris_linear_fp8_fwd(tile_rows(xq).view(torch.float8_e4m3fn), tile_rows(xs).view(torch.float8_e8m0fnu),
+                               repeat(w8).view(torch.float8_e4m3fn), repeat(ws).view(torch.float8_e8m0fnu))
+    torch.cuda.synchronize()
+    assert (y == y[:, :1]).all() and (y[:, 0] == y[:kinds, 0][kind]).all()
+    got, ref = to_f64(y[:kinds, 0]), x.sum(1)
+    most, mag = np.abs(x).reshape(kinds, -1, 8).max(2).sum(1), np.abs(x).sum(1)
+    err = np.abs(got - ref)
+    print("error / sum |x w|", (err / mag).max(), "first term", (7 * 2.0 ** -13 * most / mag).min())
+    assert (err <= 2.0 ** -8 * np.abs(ref) + 7 * 2.0 ** -13 * most + (c / 16 + 8) * 2.0 ** -23 * mag).all()
+
+
+@pytest.mark.parametrize("n,c,f,tile", [(3, 65536, 64, 16), (40, 65472, 64, 64), (129, 65536, 128, 64)])
+def test_linear_of_the_most_channels(n, c, f, tile):
+    assert B.aeris_linear_fp8_plan(n, c, f)[0] == tile
+    test_linear(n, c, f)
