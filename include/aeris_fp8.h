@@ -116,8 +116,12 @@ int aeris_linear_fp8_fwd(const void* x8, const void* xs, const void* w8, const v
  *                                        one after 8-bit products, which lose 1e-5 of it
  * Either output may be NULL (then its operands x8, xs or wt8, wts may be too).
  * Limits as in aeris_linear_fp8_fwd, and out_features * channels < 2^31.  workspace: at least
- * aeris_linear_fp8_bwd_workspace_bytes(...) bytes, contents undefined before and after.
+ * aeris_linear_fp8_bwd_workspace_bytes_for(...) bytes of the outputs that are wanted (dx alone needs
+ * room for dy in 8 bits only; aeris_linear_fp8_bwd_workspace_bytes(...) is the size for both), 0 if
+ * the size is not accepted; contents undefined before and after.
  */
+size_t aeris_linear_fp8_bwd_workspace_bytes_for(int64_t n_rows, int32_t channels, int32_t out_features,
+                                                int32_t want_dx, int32_t want_dweight);
 size_t aeris_linear_fp8_bwd_workspace_bytes(int64_t n_rows, int32_t channels, int32_t out_features);
 int aeris_linear_fp8_bwd(const void* x8, const void* xs, const void* wt8, const void* wts,
                          const void* dy, int64_t n_rows, int32_t channels, int32_t out_features,

@@ -34,7 +34,8 @@ EXPORTS = ("aeris_winattn_fwd", "aeris_winattn_bwd", "aeris_winattn_bwd_stages",
            "aeris_linear_bwd_workspace_bytes", "aeris_linear_bwd",
            # include/aeris_fp8.h
            "aeris_fp8_scale_pitch", "aeris_fp8_quantize", "aeris_residual_norm_fp8_fwd", "aeris_swiglu_fp8_fwd",
-           "aeris_linear_fp8_fwd", "aeris_linear_fp8_bwd_workspace_bytes", "aeris_linear_fp8_bwd",
+           "aeris_linear_fp8_fwd", "aeris_linear_fp8_bwd_workspace_bytes_for",
+           "aeris_linear_fp8_bwd_workspace_bytes", "aeris_linear_fp8_bwd",
            "aeris_linear_fp8_plan", "aeris_linear_fp8_parts")
 
 
@@ -173,6 +174,8 @@ def load():
     lib.aeris_swiglu_fp8_fwd.restype = ctypes.c_int
     lib.aeris_linear_fp8_fwd.argtypes = [vp, vp, vp, vp, i64, i32, i32, vp, vp]
     lib.aeris_linear_fp8_fwd.restype = ctypes.c_int
+    lib.aeris_linear_fp8_bwd_workspace_bytes_for.argtypes = [i64, i32, i32, i32, i32]
+    lib.aeris_linear_fp8_bwd_workspace_bytes_for.restype = sz
     lib.aeris_linear_fp8_bwd_workspace_bytes.argtypes = [i64, i32, i32]
     lib.aeris_linear_fp8_bwd_workspace_bytes.restype = sz
     lib.aeris_linear_fp8_bwd.argtypes = [vp, vp, vp, vp, vp, i64, i32, i32, vp, vp, vp, sz, vp]
@@ -887,6 +890,11 @@ def aeris_linear_fp8_parts(n_rows, channels, out_features):
     return out.value
 
 
+def aeris_linear_fp8_bwd_workspace_bytes_for(n_rows, channels, out_features, want_dx, want_dweight):
+    return load().aeris_linear_fp8_bwd_workspace_bytes_for(n_rows, channels, out_features, bool(want_dx),
+                                                           bool(want_dweight))
+
+
 def aeris_linear_fp8_bwd_workspace_bytes(n_rows, channels, out_features):
     return load().aeris_linear_fp8_bwd_workspace_bytes(n_rows, channels, out_features)
 
@@ -917,7 +925,8 @@ def aeris_linear_fp8_bwd(x8, xs, wt8, wts, dy, want_dx=True, want_dweight=True, 
         else:
             assert dweight.shape == (f, c) and dweight.is_contiguous() and dweight.dtype == torch.float32
     if workspace is None:
-        workspace = dy.new_empty(max(aeris_linear_fp8_bwd_workspace_bytes(n, c, f), 16), dtype=torch.uint8)
+        need = aeris_linear_fp8_bwd_workspace_bytes_for(n, c, f, want_dx, want_dweight)
+        workspace = dy.new_empty(max(need, 16), dtype=torch.uint8)
     assert workspace.is_contiguous()
     _here(dy, workspace)
     if want_dx:

@@ -821,25 +821,26 @@ int check_linear(int64_t n_rows, int32_t channels, int32_t features) {
 bool bad16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) != 0; }
 size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
-// The workspace of the gradients: x in bf16 and, behind it, what the product of dW needs; dy quantised for the product
-// of dx, which comes first, in the place of the latter where that is large enough, else of all of it.
+// The workspace of the gradients.  For dW: x in bf16 and, behind it, what its product needs.  For dx: dy quantised.  For
+// both dy comes first, in the place of what dW's product needs where that is large enough, else of all of it.
 struct Backward {
   size_t wgrad;           // offset of the workspace of the product of dW
   size_t dy, dys;         // offsets of dy's values and scales
   size_t bytes;
 };
 // AERIS_OK if both products of the backward pass accept the size, else an AERIS_ERR_ code.
-int backward_layout(int64_t n_rows, int32_t channels, int32_t features, Backward& b) {
+int backward_layout(int64_t n_rows, int32_t channels, int32_t features, bool want_dx, bool want_dw, Backward& b) {
   if (const int rc = check_linear(n_rows, features, channels)) return rc;
   if ((long long)channels * features >= (1LL << 31)) return AERIS_ERR_INVALID_SHAPE;
-  const size_t for_dw = aeris_linear_bwd_workspace_bytes(n_rows, channels, features);
-  if (for_dw == 0) return AERIS_ERR_INVALID_SHAPE;
+  const size_t product = aeris_linear_bwd_workspace_bytes(n_rows, channels, features);
+  if (product == 0) return AERIS_ERR_INVALID_SHAPE;
   b.wgrad = round256((size_t)n_rows * channels * 2);
   const size_t values = round256((size_t)n_rows * features);
-  const size_t for_dx = values + round256((size_t)n_rows * scale_pitch(features));
-  b.dy = for_dx <= for_dw ? b.wgrad : 0;
+  const size_t for_dx = want_dx ? values + round256((size_t)n_rows * scale_pitch(features)) : 0;
+  const size_t for_dw = want_dw ? b.wgrad + product : 0;
+  b.dy = want_dw && for_dx <= product ? b.wgrad : 0;
   b.dys = b.dy + values;
-  b.bytes = b.wgrad + for_dw > for_dx ? b.wgrad + for_dw : for_dx;
+  b.bytes = for_dw > for_dx ? for_dw : for_dx;
   return AERIS_OK;
 }
 
@@ -888,9 +889,15 @@ extern "C" int aeris_linear_fp8_parts(int64_t n_rows, int32_t channels, int32_t 
   return AERIS_OK;
 }
 
-extern "C" size_t aeris_linear_fp8_bwd_workspace_bytes(int64_t n_rows, int32_t channels, int32_t out_features) {
+extern "C" size_t aeris_linear_fp8_bwd_workspace_bytes_for(int64_t n_rows, int32_t channels, int32_t out_features,
+                                                           int32_t want_dx, int32_t want_dweight) {
   Backward at;
-  return backward_layout(n_rows, channels, out_features, at) == AERIS_OK ? at.bytes : 0;
+  if (backward_layout(n_rows, channels, out_features, want_dx != 0, want_dweight != 0, at) != AERIS_OK) return 0;
+  return at.bytes;
+}
+
+extern "C" size_t aeris_linear_fp8_bwd_workspace_bytes(int64_t n_rows, int32_t channels, int32_t out_features) {
+  return aeris_linear_fp8_bwd_workspace_bytes_for(n_rows, channels, out_features, 1, 1);
 }
 
 extern "C" int aeris_linear_fp8_bwd(const void* x8, const void* xs, const void* wt8, const void* wts, const void* dy,
@@ -899,7 +906,8 @@ extern "C" int aeris_linear_fp8_bwd(const void* x8, const void* xs, const void* 
   if (!dy || !workspace || (!dx && !dweight) || (dx && (!wt8 || !wts)) || (dweight && (!x8 || !xs)))
     return AERIS_ERR_NULL_POINTER;
   Backward at;
-  if (const int rc = backward_layout(n_rows, channels, out_features, at)) return rc;
+  if (const int rc = backward_layout(n_rows, channels, out_features, dx != nullptr, dweight != nullptr, at))
+    return rc;
   if (bad16(x8) || bad16(xs) || bad16(wt8) || bad16(wts) || bad16(dy) || bad16(dx) || bad16(dweight) ||
       bad16(workspace))
     return AERIS_ERR_MISALIGNED;

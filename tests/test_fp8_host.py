@@ -154,3 +154,19 @@ def test_linear_tells_its_parts():
     assert [B.aeris_linear_fp8_parts(*v) for v in ((1, 2048, 12288), (128, 5504, 2048), (172800, 2048, 11008))] == [8, 4, 1]
     with pytest.raises(B.AerisError):
         B.aeris_linear_fp8_parts(8, 96, 64)
+
+
+def test_linear_bwd_workspace_of_what_is_wanted():
+    lib = B.load()
+    up = lambda v: -(-v // 256) * 256
+    size = B.aeris_linear_fp8_bwd_workspace_bytes_for
+    for n, c, f in ((1, 64, 64), (1000, 192, 320), (40, 128, 2048), (172800, 5504, 2048)):
+        for_dx = up(n * f) + up(n * B.aeris_fp8_scale_pitch(f))
+        for_dw = up(n * c * 2) + B.aeris_linear_bwd_workspace_bytes(n, c, f)
+        assert size(n, c, f, True, False) == for_dx and size(n, c, f, False, True) == for_dw
+        assert size(n, c, f, True, True) == max(for_dx, for_dw) == B.aeris_linear_fp8_bwd_workspace_bytes(n, c, f)
+        for dx, dw in ((A, None), (None, A), (A, A)):                  # one byte less is refused
+            assert lib.aeris_linear_fp8_bwd(A, A, A, A, A, n, c, f, dx, dw, A, size(n, c, f, dx, dw) - 1, None) == -8
+    assert size(172800, 5504, 2048, True, False) < 360e6              # 2466 MB for both
+    for bad in ((0, 64, 64), (8, 100, 64), (8, 64, 72), (8, 65536, 65536)):
+        assert size(*bad, True, False) == 0 and size(*bad, False, True) == 0

@@ -726,3 +726,24 @@ def test_sums_of_many_channels_beside_a_large_block(n, c, f, tile, parts):
 def test_linear_of_the_most_channels(n, c, f, tile):
     assert B.aeris_linear_fp8_plan(n, c, f)[0] == tile
     test_linear(n, c, f)
+
+
+@pytest.mark.parametrize("n,c,f", [(40, 128, 2048), (131, 192, 576), (2125, 64, 128), (1100, 1088, 1600)])
+def test_linear_bwd_within_the_workspace_of_what_is_wanted(n, c, f):
+    """Each output alone, and both, with no byte more than is asked for and nothing written behind it."""
+    rng = np.random.default_rng(n)
+    (x8, xs), _ = operand(rng, n, c)
+    _, _, wt8, wts = B.aeris_fp8_quantize(bf16(rng.standard_normal((f, c)))[0], rows=False, transposed=True)
+    tdy, _ = bf16(rows_with_gain(rng, n, f))
+    want = B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, tdy)
+    for which in ((True, True), (True, False), (False, True)):
+        need = B.aeris_linear_fp8_bwd_workspace_bytes_for(n, c, f, *which)
+        space = torch.full((need + 4096,), 0x5a, dtype=torch.uint8, device="cuda")
+        got = B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, tdy, *which, workspace=space[:need])
+        torch.cuda.synchronize()
+        assert (space[need:] == 0x5a).all()
+        for wanted, g, w in zip(which, got, want):
+            assert torch.equal(g, w) if wanted else g is None
+        with pytest.raises(B.AerisError) as e:
+            B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, tdy, *which, workspace=space[:need - 1])
+        assert e.value.code == -8
