@@ -774,10 +774,20 @@ def aeris_fp8_scale_pitch(cols):
     return load().aeris_fp8_scale_pitch(cols)
 
 
-def _empty_quantized(x, rows, cols):
+def _out_quantized(x, rows, cols, q, scales):
+    """Where a quantised [rows, cols] goes: the tensors passed in, checked, or new ones beside x."""
     import torch
-    return (x.new_empty((rows, cols), dtype=torch.float8_e4m3fn),
-            x.new_empty((rows, (cols + 511) // 512 * 4), dtype=torch.float8_e8m0fnu))
+    pitch = (cols + 511) // 512 * 4
+    if q is None:
+        q = x.new_empty((rows, cols), dtype=torch.float8_e4m3fn)
+    else:
+        assert q.dtype == torch.float8_e4m3fn and q.is_contiguous() and q.shape == (rows, cols) and q.device == x.device
+    if scales is None:
+        scales = x.new_empty((rows, pitch), dtype=torch.float8_e8m0fnu)
+    else:
+        assert (scales.dtype == torch.float8_e8m0fnu and scales.is_contiguous() and scales.shape == (rows, pitch)
+                and scales.device == x.device)
+    return q, scales
 
 
 def _here(*tensors):
@@ -796,15 +806,22 @@ def _quantized(q, scales):
     return n, c
 
 
-def aeris_fp8_quantize(x, rows=True, transposed=False):
+def aeris_fp8_quantize(x, rows=True, transposed=False, x8=None, xs=None, xt8=None, xts=None):
     """x [n, C] bf16 or fp32.  Returns (x8, xs, xt8, xts): x quantised by rows and its transpose
-    quantised by rows; entries not asked for are None."""
+    quantised by rows, allocated unless passed in; entries not asked for are None (and must not be
+    passed in)."""
     import torch
     assert x.is_contiguous() and x.dim() == 2 and x.dtype in (torch.bfloat16, torch.float32)
     _here(x)
     n, c = x.shape
-    x8, xs = _empty_quantized(x, n, c) if rows else (None, None)
-    xt8, xts = _empty_quantized(x, c, n) if transposed else (None, None)
+    if rows:
+        x8, xs = _out_quantized(x, n, c, x8, xs)
+    else:
+        assert x8 is None and xs is None
+    if transposed:
+        xt8, xts = _out_quantized(x, c, n, xt8, xts)
+    else:
+        assert xt8 is None and xts is None
     rc = load().aeris_fp8_quantize(x.data_ptr(), AERIS_DT_F32 if x.dtype == torch.float32 else AERIS_DT_BF16,
                                    n, c, _ptr(x8), _ptr(xs), _ptr(xt8), _ptr(xts), _stream())
     if rc != 0:
@@ -812,9 +829,10 @@ def aeris_fp8_quantize(x, rows=True, transposed=False):
     return x8, xs, xt8, xts
 
 
-def aeris_residual_norm_fp8_fwd(x, y, alpha, w, gamma, beta, eps, rows_per_sample, s=None, want_r=True):
+def aeris_residual_norm_fp8_fwd(x, y, alpha, w, gamma, beta, eps, rows_per_sample, s=None, want_r=True, r=None,
+                                h8=None, hs=None):
     """s = x + alpha_b * y, h = RMSNorm(s; w) * (1 + gamma_b) + beta_b.  Returns (s, r, h8, hs); with y None
-    nothing is added and s is x.  s may be passed in, also as x or y."""
+    nothing is added and s is x.  Results may be passed in, s also as x or y."""
     import torch
     n, c = _rows(x)
     _f32(w, gamma, beta, alpha)
@@ -831,8 +849,11 @@ def aeris_residual_norm_fp8_fwd(x, y, alpha, w, gamma, beta, eps, rows_per_sampl
         assert w.numel() == c and gamma.numel() == beta.numel() == per_sample
         assert y is None or alpha is None or alpha.numel() == per_sample
     _here(x, y, alpha, w, gamma, beta, s)
-    r = x.new_empty(n, dtype=torch.float32) if want_r else None
-    h8, hs = _empty_quantized(x, n, c)
+    if r is None:
+        r = x.new_empty(n, dtype=torch.float32) if want_r else None
+    else:
+        assert r.dtype == torch.float32 and r.is_contiguous() and r.shape == (n,) and r.device == x.device
+    h8, hs = _out_quantized(x, n, c, h8, hs)
     rc = load().aeris_residual_norm_fp8_fwd(x.data_ptr(), _ptr(y), _ptr(alpha), w.data_ptr(), gamma.data_ptr(),
                                             beta.data_ptr(), float(eps), n, rows_per_sample, c,
                                             None if y is None else s.data_ptr(), _ptr(r), h8.data_ptr(),
@@ -842,12 +863,12 @@ def aeris_residual_norm_fp8_fwd(x, y, alpha, w, gamma, beta, eps, rows_per_sampl
     return s, r, h8, hs
 
 
-def aeris_swiglu_fp8_fwd(uv):
-    """(g8, gs): g = silu(u) * v for uv = [u | v], quantised."""
+def aeris_swiglu_fp8_fwd(uv, g8=None, gs=None):
+    """(g8, gs): g = silu(u) * v for uv = [u | v], quantised; allocated unless passed in."""
     n, c2 = _rows(uv)
     assert c2 % 2 == 0
     _here(uv)
-    g8, gs = _empty_quantized(uv, n, c2 // 2)
+    g8, gs = _out_quantized(uv, n, c2 // 2, g8, gs)
     rc = load().aeris_swiglu_fp8_fwd(uv.data_ptr(), n, c2 // 2, g8.data_ptr(), gs.data_ptr(), _stream())
     if rc != 0:
         raise AerisError(rc, "aeris_swiglu_fp8_fwd")

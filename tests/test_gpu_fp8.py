@@ -747,3 +747,46 @@ def test_linear_bwd_within_the_workspace_of_what_is_wanted(n, c, f):
         with pytest.raises(B.AerisError) as e:
             B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, tdy, *which, workspace=space[:need - 1])
         assert e.value.code == -8
+
+
+# ------------------------------------------------------------------------------------- results passed in
+def results_of_each_call():
+    """(call with keyword arguments for its results, names of the results, those of a call without)."""
+    rng = np.random.default_rng(61)
+    t, _ = bf16(rows_with_gain(rng, 128, 192))
+    y, _ = bf16(rows_with_gain(rng, 128, 192))
+    uv, _ = bf16(rows_with_gain(rng, 128, 384))
+    ta, tw, tg, tb = [f32(rng.standard_normal(v))[0] for v in ((2, 192), 192, (2, 192), (2, 192))]
+    quantize = lambda **kw: B.aeris_fp8_quantize(t, transposed=True, **kw)
+    norm = lambda **kw: B.aeris_residual_norm_fp8_fwd(t, y, ta, tw, tg, tb, 1e-6, 64, **kw)
+    gate = lambda **kw: B.aeris_swiglu_fp8_fwd(uv, **kw)
+    return [(call, names, call()) for call, names in (
+        (quantize, ("x8", "xs", "xt8", "xts")), (norm, ("s", "r", "h8", "hs")), (gate, ("g8", "gs")))]
+
+
+def test_results_passed_in():
+    """All of them and each alone: written to the bits of a call that allocates, and returned as they are."""
+    raw = lambda v: v.view(torch.uint8)
+    for call, names, want in results_of_each_call():
+        for given in (names,) + tuple((n,) for n in names):
+            outs = {n: torch.empty_like(w) for n, w in zip(names, want) if n in given}
+            for o in outs.values():
+                raw(o).fill_(0x33)
+            got = call(**outs)
+            torch.cuda.synchronize()
+            for name, g, w in zip(names, got, want):
+                assert torch.equal(raw(g), raw(w)) and (name not in outs or g is outs[name])
+
+
+def test_results_passed_in_are_refused_where_they_do_not_fit():
+    for call, names, want in results_of_each_call():
+        for name, w in zip(names, want):
+            wide = torch.empty((2 * w.shape[0],) + w.shape[1:], dtype=w.dtype, device="cuda")
+            for bad in (w[:-1], wide, wide[::2], torch.empty_like(w, dtype=torch.float16), w.cpu()):
+                with pytest.raises(AssertionError):
+                    call(**{name: bad})
+    x = torch.zeros(64, 64, dtype=torch.bfloat16, device="cuda")
+    x8, xs, xt8, xts = B.aeris_fp8_quantize(x, transposed=True)
+    for kw in (dict(rows=False, transposed=True, x8=x8), dict(rows=False, transposed=True, xs=xs), dict(xt8=xt8), dict(xts=xts)):
+        with pytest.raises(AssertionError):
+            B.aeris_fp8_quantize(x, **kw)
