@@ -831,12 +831,14 @@ def aeris_fp8_quantize(x, rows=True, transposed=False, x8=None, xs=None, xt8=Non
 
 def aeris_residual_norm_fp8_fwd(x, y, alpha, w, gamma, beta, eps, rows_per_sample, s=None, want_r=True, r=None,
                                 h8=None, hs=None):
-    """s = x + alpha_b * y, h = RMSNorm(s; w) * (1 + gamma_b) + beta_b.  Returns (s, r, h8, hs); with y None
-    nothing is added and s is x.  Results may be passed in, s also as x or y."""
+    """s = x + alpha_b * y, h = RMSNorm(s; w) * (1 + gamma_b) + beta_b.  Returns (s, r, h8, hs).  Results may be
+    passed in, s also as x or y.  With y None nothing is added: s is x (nothing else can be passed in for it),
+    and alpha is not read."""
     import torch
     n, c = _rows(x)
     _f32(w, gamma, beta, alpha)
     if y is None:
+        assert s is None or s is x                       # a buffer of its own would not be written
         s = x
     else:
         assert _rows(y) == (n, c)

@@ -790,3 +790,16 @@ def test_results_passed_in_are_refused_where_they_do_not_fit():
     for kw in (dict(rows=False, transposed=True, x8=x8), dict(rows=False, transposed=True, xs=xs), dict(xt8=xt8), dict(xts=xts)):
         with pytest.raises(AssertionError):
             B.aeris_fp8_quantize(x, **kw)
+
+
+def test_norm_without_residual_refuses_a_sum_of_its_own():
+    """Without y nothing is written to s, so that a buffer passed in for it would stay as it was; alpha is not read."""
+    rng = np.random.default_rng(67)
+    t, _ = bf16(rows_with_gain(rng, 8, 64))
+    ta, tw, tg, tb = [f32(rng.standard_normal(v))[0] for v in ((2, 64), 64, (2, 64), (2, 64))]
+    call = lambda alpha=None, **kw: B.aeris_residual_norm_fp8_fwd(t, None, alpha, tw, tg, tb, 1e-6, 4, **kw)
+    with pytest.raises(AssertionError):
+        call(s=torch.empty_like(t))
+    want = call()
+    for got in (call(s=t), call(alpha=ta), call(alpha=torch.full_like(ta, float("nan")))):
+        assert got[0] is t and all(same_bits(g, w) for g, w in zip(got, want))
