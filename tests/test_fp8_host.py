@@ -170,3 +170,27 @@ def test_linear_bwd_workspace_of_what_is_wanted():
     assert size(172800, 5504, 2048, True, False) < 360e6              # 2466 MB for both
     for bad in ((0, 64, 64), (8, 100, 64), (8, 64, 72), (8, 65536, 65536)):
         assert size(*bad, True, False) == 0 and size(*bad, False, True) == 0
+
+
+def test_a_wrong_gradient_shows_along_itself():
+    """The check that the GPU's gradients go through (gradient_check.py) passes the oracle's, with its forward products
+    rounded to bf16, and fails a gradient of zeros and those that lack 64 features or 64 tokens of their sum."""
+    import gradient_check as gc
+    half_step = lambda rng, a: a * (1 + 2.0 ** -8 * rng.uniform(-1, 1, a.shape))
+    for n, c, f in ((96, 256, 192), (333, 192, 320), (500, 448, 576)):
+        rng = np.random.default_rng(n + c + f)
+        rows = lambda r, k: fo.round_trip(rng.standard_normal((r, k)) * np.exp(rng.standard_normal(k)))
+        x, dy, weight = rows(n, c), rows(n, f), rng.standard_normal((f, c)) / np.sqrt(c)
+        w, wt = fo.round_trip(weight), fo.round_trip(weight.T)
+        dx, dw = fo.linear_bwd(x, wt, dy)
+        u, v = fo.round_trip(dx), fo.round_trip(dw)
+        along_dx = lambda dx: gc.along_dx(half_step(rng, fo.linear_fwd(u, w)), dx, u, dy, w, wt)
+        along_dw = lambda dw: gc.along_dw(half_step(rng, fo.linear_fwd(x, v)), dw, v, dy, x)
+        for along, right, wrong in (
+                (along_dx, half_step(rng, dx), [0 * dx, fo.linear_bwd(x, wt[:, 64:], dy[:, 64:])[0]]),
+                (along_dw, dw, [0 * dw, fo.linear_bwd(x[64:], wt, dy[64:])[1]])):
+            gap, allow, size = along(right)
+            assert gap <= allow <= 0.02 * size
+            for g in wrong:
+                gap, allow, _ = along(g)
+                assert gap > 2 * allow

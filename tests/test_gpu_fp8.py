@@ -17,6 +17,7 @@ from oracle import block_oracle as bo
 from oracle import fp8_oracle as fo
 from paper_2509_13523_amd import binding as B
 from paper_2509_13523_amd import synth
+import gradient_check as gc
 import parity_log
 
 pytestmark = pytest.mark.gpu
@@ -803,3 +804,26 @@ def test_norm_without_residual_refuses_a_sum_of_its_own():
     want = call()
     for got in (call(s=t), call(alpha=ta), call(alpha=torch.full_like(ta, float("nan")))):
         assert got[0] is t and all(same_bits(g, w) for g, w in zip(got, want))
+
+
+@pytest.mark.parametrize("n,c,f", [(96, 256, 192), (17, 1088, 64), (333, 192, 320), (500, 448, 576), (2500, 1600, 2112)])
+def test_linear_gradients_along_themselves(n, c, f):
+    """The library's gradients against its own forward products along them (gradient_check.py says what is allowed;
+    test_a_wrong_gradient_shows_along_itself that wrong ones fail).  A gradient that lacks 64 terms of its sum is off by
+    about 64 / terms of what is compared: less than that is allowed.  What is allowed grows with the square root of the
+    terms (sums of magnitudes beside a sum of either sign): 0.8 % at 192, 2.0 % at 2112, 2.1 % at 2500 of them."""
+    rng = np.random.default_rng(n + c + f)
+    (x8, xs), x = operand(rng, n, c)
+    tw, _ = bf16(rng.standard_normal((f, c)) / np.sqrt(c))
+    w8, ws, wt8, wts = B.aeris_fp8_quantize(tw, transposed=True)
+    tdy, dy = bf16(fo.round_trip(rows_with_gain(rng, n, f)))              # quantising it again changes nothing
+    assert (fo.round_trip(dy) == dy).all()
+    dx, dw = (to_f64(g) for g in B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, tdy))
+    u, v = fo.quantize(dx), fo.quantize(dw)
+    along_u = to_f64(B.aeris_linear_fp8_fwd(*dev(*u), w8, ws))
+    along_v = to_f64(B.aeris_linear_fp8_fwd(x8, xs, *dev(*v)))
+    w, wt = fo.dequantize(*codes(w8, ws)), fo.dequantize(*codes(wt8, wts))
+    for (gap, allow, size), terms in ((gc.along_dx(along_u, dx, fo.dequantize(*u), dy, w, wt), f),
+                                      (gc.along_dw(along_v, dw, fo.dequantize(*v), dy, x), n)):
+        print("gap %.3e allowed %.3e of %.3e" % (gap, allow, size))
+        assert gap <= allow <= min(0.05, 64 / terms) * size
