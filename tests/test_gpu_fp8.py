@@ -827,3 +827,145 @@ def test_linear_gradients_along_themselves(n, c, f):
                                       (gc.along_dw(along_v, dw, fo.dequantize(*v), dy, x), n)):
         print("gap %.3e allowed %.3e of %.3e" % (gap, allow, size))
         assert gap <= allow <= min(0.05, 64 / terms) * size
+
+
+# ------------------------------------------------------------------------------------- every form
+def drawn_operand(gen, n, c):
+    """A quantised matrix drawn on the device."""
+    gain = torch.randn(c, device="cuda", generator=gen).exp()
+    x = torch.randn(n, c, device="cuda", generator=gen) * gain
+    return B.aeris_fp8_quantize(x)[:2]
+
+
+def drawn_values(q, scales):
+    """What it stands for, exact in bf16."""
+    power = torch.exp2(scales.view(torch.uint8).float() - 127.0).repeat_interleave(128, 1)[:, :q.shape[1]]
+    return (q.float() * power).bfloat16()
+
+
+def sampled(rng, n, side):
+    """Where tiles meet and end, and more."""
+    edges = [0, 1, side - 1, side, n - side - 1, n - side, n - 2, n - 1]
+    return np.unique(np.clip(np.concatenate([edges, rng.integers(0, n, 40)]), 0, n - 1))
+
+
+@pytest.mark.parametrize("n,c,f,dx_form,dw_side,together", [
+    (65, 1344, 2368, (64, 4), 128, True), (849, 2368, 128, (128, 1), 64, True), (16435, 128, 64, (128, 1), 64, False),
+    (2435, 1152, 960, (128, 1), 128, True), (18569, 128, 2240, (128, 2), 128, False), (21193, 192, 1920, (128, 1), 128, False),
+    (2241, 2432, 1728, (128, 1), 256, True), (8047, 1856, 256, (256, 1), 64, True), (99835, 256, 320, (256, 1), 64, False),
+    (16207, 960, 448, (256, 1), 128, True), (114803, 448, 320, (256, 1), 128, False), (20701, 448, 1472, (256, 1), 256, True),
+    (8445, 1024, 1600, (256, 1), 256, True), (116309, 448, 448, (256, 1), 256, False), (104617, 256, 832, (256, 1), 256, False)])
+def test_linear_bwd_of_every_form(n, c, f, dx_form, dw_side, together):
+    """Both gradients in each form of dx and side of dW's tiles, with dy's 8-bit rows inside dW's workspace, which dW's
+    partial sums take over from them (`together`), and in the place of all of it; rows, channels and features past tiles."""
+    assert (B.aeris_linear_fp8_plan(n, f, c)[0], B.aeris_linear_fp8_parts(n, f, c)) == dx_form
+    assert B.aeris_linear_bwd_plan(n, c, f)[0] == dw_side
+    for_dx = B.aeris_linear_fp8_bwd_workspace_bytes_for(n, c, f, True, False)
+    assert (for_dx <= B.aeris_linear_bwd_workspace_bytes(n, c, f)) == together
+    rng, gen = np.random.default_rng(n), torch.Generator(device="cuda").manual_seed(n)
+    x8, xs = drawn_operand(gen, n, c)
+    tw = torch.randn(f, c, device="cuda", generator=gen).bfloat16()
+    _, _, wt8, wts = B.aeris_fp8_quantize(tw, rows=False, transposed=True)
+    tdy = (torch.randn(n, f, device="cuda", generator=gen) * torch.randn(f, device="cuda", generator=gen).exp()).bfloat16()
+    dx, dw = B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, tdy)
+    torch.cuda.synchronize()
+    # dx: sampled rows and channels against the oracle
+    rows, cols, feats = sampled(rng, n, dx_form[0]), sampled(rng, c, dx_form[0]), sampled(rng, f, dw_side)
+    wt = fo.dequantize(*codes(wt8[cols], wts.view(torch.uint8)[cols].view(torch.float8_e8m0fnu)))
+    close_product("dx", dx[rows][:, cols], fo.round_trip(to_f64(tdy[rows])), wt)
+    # dW: the bits of the bf16 gradient of the same values, and sampled entries against sums in 64 bits
+    values = drawn_values(x8, xs)
+    _, want = B.aeris_linear_bwd(values, tw, tdy, want_dx=False)
+    assert torch.equal(dw, want)
+    x, dy = to_f64(values[:, cols]), to_f64(tdy[:, feats])
+    err = np.abs(to_f64(dw[feats][:, cols]) - dy.T @ x)
+    assert (err <= max(1e-5, 4.0 * np.sqrt(n) * 2.0 ** -24) * (np.abs(dy).T @ np.abs(x))).all()
+    # each alone and again: the same bits
+    dx2, _ = B.aeris_linear_fp8_bwd(None, None, wt8, wts, tdy, want_dweight=False)
+    _, dw2 = B.aeris_linear_fp8_bwd(x8, xs, None, None, tdy, want_dx=False)
+    again = B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, tdy)
+    assert same_bits(dx, dx2) and same_bits(dw, dw2) and same_bits((dx, dw), again)
+
+
+@pytest.mark.parametrize("n,c,f,form", [
+    (40, 1216, 192, (16, 8)), (1000, 64, 2048, (64, 1)), (200, 1344, 128, (64, 4)), (4100, 192, 1088, (128, 1)),
+    (2500, 1600, 2112, (128, 1)), (1990, 1344, 1984, (128, 2)), (16310, 192, 832, (256, 1)), (8178, 320, 1920, (256, 1)),
+    (8085, 576, 2048, (256, 1)), (24740, 512, 960, (256, 1))])
+def test_linear_keeps_nan_to_itself_in_every_form(n, c, f, form):
+    """Values that are not numbers at both ends of the channels, in rows and features where tiles end: their rows and
+    features are, all others have the bits they have without them.  The largest scales of a row change no other."""
+    assert (B.aeris_linear_fp8_plan(n, c, f)[0], B.aeris_linear_fp8_parts(n, c, f)) == form
+    gen = torch.Generator(device="cuda").manual_seed(n + c)
+    x8, xs = drawn_operand(gen, n, c)
+    w8, ws = drawn_operand(gen, f, c)
+    want = B.aeris_linear_fp8_fwd(x8, xs, w8, ws)
+    assert torch.isfinite(want).all()
+    raw = lambda t: t.view(torch.uint8)
+    rows, feats, scaled = [(0, 0), (n // 2, c - 1), (n - 1, c // 2)], [(f // 3, 0), (f - 1, c - 1)], n // 4
+    for row, channel in rows:
+        raw(x8)[row, channel] = 0x7f
+    for feature, channel in feats:
+        raw(w8)[feature, channel] = 0xff
+    raw(xs)[scaled, 0] = 227                              # 2^100
+    y = B.aeris_linear_fp8_fwd(x8, xs, w8, ws)
+    torch.cuda.synchronize()
+    bad = torch.zeros(n, f, dtype=torch.bool, device="cuda")
+    for row, _ in rows:
+        bad[row] = True
+    for feature, _ in feats:
+        bad[:, feature] = True
+    assert torch.equal(torch.isnan(y), bad)
+    bad[scaled] = True
+    assert torch.equal(y.view(torch.int16)[~bad], want.view(torch.int16)[~bad])
+
+
+LARGE_GRADIENTS = [(20701, 448, 1472), (104617, 256, 832), (18569, 128, 2240), (2241, 2432, 1728)]
+
+
+def gradient_operands(gen, n, c, f):
+    x8, xs = drawn_operand(gen, n, c)
+    w = torch.randn(f, c, device="cuda", generator=gen).bfloat16()
+    w8, ws, wt8, wts = B.aeris_fp8_quantize(w, transposed=True)
+    return [x8, xs, w8, ws, wt8, wts, torch.randn(n, f, device="cuda", generator=gen).bfloat16()]
+
+
+@pytest.mark.parametrize("n,c,f", LARGE_GRADIENTS)
+def test_linear_bwd_keeps_what_is_not_finite_to_itself(n, c, f):
+    gen = torch.Generator(device="cuda").manual_seed(n)
+    x8, xs, _, _, wt8, wts, dy = gradient_operands(gen, n, c, f)
+    dx, dw = B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, dy)
+    dy[n // 2, f - 1], dy[n - 1, 0] = float("inf"), float("nan")
+    x8.view(torch.uint8)[n // 3, c - 1] = 0x7f
+    dx2, dw2 = B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, dy)
+    torch.cuda.synchronize()
+    bad = torch.zeros(n, c, dtype=torch.bool, device="cuda")
+    bad[n // 2], bad[n - 1] = True, True
+    assert torch.equal(~torch.isfinite(dx2), bad) and torch.equal(dx[~bad], dx2[~bad])
+    bad = torch.zeros(f, c, dtype=torch.bool, device="cuda")
+    bad[f - 1], bad[0], bad[:, c - 1] = True, True, True
+    assert torch.equal(~torch.isfinite(dw2), bad) and torch.equal(dw[~bad], dw2[~bad])
+
+
+def test_captured_products_and_gradients_of_many_tiles():
+    """The largest forms and both layouts of the gradients' workspace in one graph, replayed with new inputs in place."""
+    gen = torch.Generator(device="cuda").manual_seed(71)
+
+    def call(x8, xs, w8, ws, wt8, wts, dy):
+        return (B.aeris_linear_fp8_fwd(x8, xs, w8, ws),) + B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, dy)
+    held = [gradient_operands(gen, *size) for size in LARGE_GRADIENTS]
+    assert {B.aeris_linear_fp8_plan(n, c, f)[0] for n, c, f in LARGE_GRADIENTS} == {128, 256}
+    for v in held:
+        call(*v)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = [call(*v) for v in held]
+    for _ in range(3):
+        for v, size in zip(held, LARGE_GRADIENTS):
+            for old, new in zip(v, gradient_operands(gen, *size)):
+                old.view(torch.uint8).copy_(new.view(torch.uint8))
+        want = [call(*v) for v in held]
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(same_bits(a, b) for a, b in zip(outs, want))
+        torch.randn(1000, 1000, device="cuda").sum().item()
