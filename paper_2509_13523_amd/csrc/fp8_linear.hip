@@ -54,7 +54,6 @@ struct LinearShape {
   static constexpr int kStageBytes = kScaleAt + (kBM + kBN) * 4;
   static constexpr int kSmem = kStages * kStageBytes;
 };
-using LinearLarge = LinearShape<2, 2, 4, 4, 2>;    // 256 x 256, one workgroup per CU
 using LinearMedium = LinearShape<2, 2, 2, 2, 2>;   // 128 x 128, two workgroups per CU
 using LinearSmall = LinearShape<2, 1, 1, 2, 4>;    // 64 x 64, two workgroups per CU, three stages in flight
 // one workgroup per CU: groups of waves share the channels
@@ -91,12 +90,6 @@ __device__ __forceinline__ f32x16 mfma_e4m3(i32x8 a, i32x8 b, f32x16 c, int scal
   return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, c, 0, 0, 0, scale_a, 0, scale_b);
 }
 
-__device__ __forceinline__ i32x8 read_pair(uint32_t lo, uint32_t hi) {
-  const i32x4 a = *reinterpret_cast<const AERIS_LDS i32x4*>(lo);
-  const i32x4 b = *reinterpret_cast<const AERIS_LDS i32x4*>(hi);
-  return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-}
-
 // Four bytes per lane, global -> LDS; executed only if `enable` (wave-uniform) is non-zero.
 __device__ __forceinline__ void async_copy4_off(uint32_t offset, unsigned long long base, uint32_t lds_base,
                                                 uint32_t enable) {
@@ -120,17 +113,16 @@ __device__ __forceinline__ unsigned long long uniform(const void* ptr) {
          (uint32_t)__builtin_amdgcn_readfirstlane((int)a);
 }
 
-// read_pair() with a constant distance behind the addresses, which goes into the instructions.
-__device__ __forceinline__ i32x8 read_tile(uint32_t lo, uint32_t hi, int behind) {
+// 32 bytes of an operand row, its chunks at `lo` and `hi`, and a scale; a constant distance behind the addresses goes
+// into the instructions.
+__device__ __forceinline__ i32x8 read_tile(uint32_t lo, uint32_t hi, int behind = 0) {
   const i32x4 a = *reinterpret_cast<const AERIS_LDS i32x4*>(reinterpret_cast<const AERIS_LDS char*>(lo) + behind);
   const i32x4 b = *reinterpret_cast<const AERIS_LDS i32x4*>(reinterpret_cast<const AERIS_LDS char*>(hi) + behind);
   return __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
 }
-__device__ __forceinline__ int scale_behind(uint32_t lds, int behind) {
+__device__ __forceinline__ int read_scale(uint32_t lds, int behind = 0) {
   return *(reinterpret_cast<const AERIS_LDS unsigned char*>(lds) + behind);
 }
-
-__device__ __forceinline__ int scale_at(uint32_t lds) { return *reinterpret_cast<const AERIS_LDS unsigned char*>(lds); }
 
 // Results of the wave (wm, wn), NB * 32 token rows x 64 features, through its own region at `stage` of the LDS
 // (128-byte rows, 16-byte chunks XORed with the row), two blocks of rows at a time, out in 16-byte pieces,
@@ -267,19 +259,19 @@ __global__ __launch_bounds__(Sh::kWaves * G * 64, 2) void fp8_linear_kernel(Line
     if (G > 1 && later < 0) break;                     // only ever in the last of all
     int scale_w[2], scale_x[NB];
 #pragma unroll
-    for (int a = 0; a < 2; ++a) scale_w[a] = scale_at(sa + here + a * 128 + (ks & 3));
+    for (int a = 0; a < 2; ++a) scale_w[a] = read_scale(sa + here + a * 128 + (ks & 3));
 #pragma unroll
-    for (int b = 0; b < NB; ++b) scale_x[b] = scale_at(sb + here + b * 128 + (ks & 3));
+    for (int b = 0; b < NB; ++b) scale_x[b] = read_scale(sb + here + b * 128 + (ks & 3));
 #pragma unroll
     for (int m = 0; m < 2; ++m) {
       if (m == 1 && half && ks == k_steps - 1) break;
       i32x8 w[2], x[NB];
 #pragma unroll
       for (int a = 0; a < 2; ++a)
-        w[a] = read_pair(va[2 * m] + here + a * 4096, va[2 * m + 1] + here + a * 4096);
+        w[a] = read_tile(va[2 * m] + here + a * 4096, va[2 * m + 1] + here + a * 4096);
 #pragma unroll
       for (int b = 0; b < NB; ++b)
-        x[b] = read_pair(vb[2 * m] + here + b * 4096, vb[2 * m + 1] + here + b * 4096);
+        x[b] = read_tile(vb[2 * m] + here + b * 4096, vb[2 * m + 1] + here + b * 4096);
 #pragma unroll
       for (int a = 0; a < 2; ++a)
 #pragma unroll
@@ -493,11 +485,11 @@ __global__ __launch_bounds__(256, 1) void fp8_linear_large_kernel(LinearParams p
   };
   auto read_w = [&](int a, const At& at) __attribute__((always_inline)) {
     w[a] = read_tile(at.w[0], at.w[1], a * 2048);
-    scale_w[a] = scale_behind(at.sw, a * 64);
+    scale_w[a] = read_scale(at.sw, a * 64);
   };
   auto read_x = [&](int h, int b, const At& at) __attribute__((always_inline)) {
     x[h][b] = read_tile(at.x[0], at.x[1], (4 * h + b) * 2048);
-    scale_x[h][b] = scale_behind(at.sx, (4 * h + b) * 64);
+    scale_x[h][b] = read_scale(at.sx, (4 * h + b) * 64);
   };
 
   f32x4 acc[8][8];                                     // [16 features][16 token rows]
@@ -710,21 +702,22 @@ template <class Sh, int G = 1>
 int launch_linear_shape(LinearParams p, hipStream_t stream) {
   p.n_tiles = (p.F + Sh::kBN - 1) / Sh::kBN;
   p.m_tiles = (int)((p.n_rows + Sh::kBM - 1) / Sh::kBM);
-  const unsigned tiles = (unsigned)p.m_tiles * (unsigned)p.n_tiles;
-  if constexpr (std::is_same<Sh, LinearLarge>::value) {
-    // one workgroup per CU, which walks its tiles; an XCD may have more than its eighth of them
-    const unsigned items = p.interleave ? (unsigned)((p.m_tiles + 7) / 8 * 8) * (unsigned)p.n_tiles : tiles;
-    auto launch = [&](auto half) {
-      constexpr auto kernel = fp8_linear_large_kernel<decltype(half)::value>;
-      if (!allow_full_lds<kernel>()) return -1;
-      return launch_kernel(kernel, dim3(items > kCus ? kCus : items), dim3(256), (size_t)kLargeSmem, stream, p);
-    };
-    return p.K % kStep != 0 ? launch(std::true_type{}) : launch(std::false_type{});
-  } else {
-    if (!allow_full_lds<fp8_linear_kernel<Sh, G>>()) return -1;
-    return launch_kernel(fp8_linear_kernel<Sh, G>, dim3(tiles), dim3(Sh::kWaves * G * 64), (size_t)(G * Sh::kSmem),
-                         stream, p);
-  }
+  const dim3 grid((unsigned)p.m_tiles * (unsigned)p.n_tiles), block(Sh::kWaves * G * 64);
+  if (!allow_full_lds<fp8_linear_kernel<Sh, G>>()) return -1;
+  return launch_kernel(fp8_linear_kernel<Sh, G>, grid, block, (size_t)(G * Sh::kSmem), stream, p);
+}
+
+int launch_linear_large(LinearParams p, hipStream_t stream) {
+  p.n_tiles = (p.F + kLargeSide - 1) / kLargeSide;
+  p.m_tiles = (int)((p.n_rows + kLargeSide - 1) / kLargeSide);
+  // one workgroup per CU, which walks its tiles; an XCD may have more than its eighth of them
+  const unsigned tiles = (unsigned)(p.interleave ? (p.m_tiles + 7) / 8 * 8 : p.m_tiles) * (unsigned)p.n_tiles;
+  auto launch = [&](auto half) {
+    constexpr auto kernel = fp8_linear_large_kernel<decltype(half)::value>;
+    if (!allow_full_lds<kernel>()) return -1;
+    return launch_kernel(kernel, dim3(tiles > kCus ? kCus : tiles), dim3(256), (size_t)kLargeSmem, stream, p);
+  };
+  return p.K % kStep != 0 ? launch(std::true_type{}) : launch(std::false_type{});
 }
 
 // Microseconds a shape takes: rounds of `slots` workgroups, each a fixed part and a part per step, a last round that
@@ -807,7 +800,7 @@ int launch_linear(LinearParams p, hipStream_t stream) {
     case LinearTile::kMedium: return launch_linear_shape<LinearMedium>(p, stream);
     default:
       p.interleave = interleave_large(p.n_rows, p.F);
-      return launch_linear_shape<LinearLarge>(p, stream);
+      return launch_linear_large(p, stream);
   }
 }
 
@@ -818,7 +811,6 @@ int check_linear(int64_t n_rows, int32_t channels, int32_t features) {
   return (n_rows + 63) / 64 * (features / 64) < (1LL << 25) ? AERIS_OK : AERIS_ERR_INVALID_SHAPE;
 }
 
-bool bad16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) != 0; }
 size_t round256(size_t n) { return (n + 255) & ~(size_t)255; }
 
 // The workspace of the gradients.  For dW: x in bf16 and, behind it, what its product needs.  For dx: dy quantised.  For

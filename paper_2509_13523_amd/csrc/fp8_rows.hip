@@ -515,7 +515,6 @@ int64_t chunks_per_sample(int64_t n_samples, int64_t rows_per_sample, int channe
   return chunks < most ? chunks : most;
 }
 
-bool bad16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) != 0; }
 int status(int launch_rc) { return launch_rc == 0 ? AERIS_OK : AERIS_ERR_HIP_LAUNCH; }
 
 // Calls f(Const<K>, Const<L>): vectors of eight channels per lane that hold a row, lanes of a row.

@@ -7,6 +7,8 @@
 
 namespace aeris {
 
+inline bool bad16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) != 0; }
+
 // AERIS_OK if a quantised matrix may have this size, else an AERIS_ERR_ code.
 int fp8_check(int64_t n_rows, int64_t cols);
 // 0 on success, -1 if the launch failed.
