@@ -179,10 +179,10 @@ __device__ __forceinline__ void linear_clear(f32x16 (&acc)[2][NB]) {
 // 4096 x 2048 -> 2048 21 / 39, 1024 x 768 -> 2304 7.2 / 10.2, 512 x 768 -> 2304 6.9 / 6.8.
 // G groups of Sh::kWaves waves share the channels of the tile: each takes a contiguous part of the steps, with stages
 // of its own, and the first adds the others' sums to its own in their order.  For no more tiles than CUs, where a step
-// is its instructions and latencies (64 x 64: 0.5 us) and nothing else runs beside it.  64 x 64, four groups: 128 rows x
-// 5504 -> 2048 21.2 -> 14.6 us, x 2048 -> 2048 10.1 -> 7.1, x 768 -> 2304 6.1 -> 5.5 (two groups with four stages each
-// 14.9, 7.9, 5.5; three with three 14.4, 7.9, 5.5); 128 x 128, two groups: 2048 rows x 5504 -> 2048 33.3 -> 29.6,
-// x 2048 -> 2048 15.6 -> 14.4.
+// is its instructions and latencies (64 x 64: 0.5 us) and nothing else runs beside it.  us, calls on two sets of operands
+// in turn: 64 x 64, four groups: 128 rows x 5504 -> 2048 21.2 -> 14.8 (on one set, which stays in the L2s, 21.0 -> 12.4),
+// x 2048 -> 2048 10.1 -> 7.2, x 768 -> 2304 6.1 -> 5.6 (two groups with four stages each 14.9, 7.9, 5.5; three with three
+// 14.4, 7.9, 5.5); 128 x 128, two groups: 2048 rows x 5504 -> 2048 35.3 -> 31.3, x 2048 -> 2048 15.5 -> 14.4.
 template <class Sh, int G>
 __global__ __launch_bounds__(Sh::kWaves * G * 64, 2) void fp8_linear_kernel(LinearParams p) {
   constexpr int kBN = Sh::kBN, NB = Sh::NB, W = Sh::kWaves, kStages = Sh::kStages;
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(Sh::kWaves * G * 64, 2) void fp8_linear_kernel(Line
 // store at a time: 20,011 x 768 -> 2304 44 us (stores among products 47, past the caches 48), at 2.4 GHz.  Per call,
 // us, eight waves of two SIMD mates in turns (the scheme of the bf16 projections) / this: 172,800 x 2048 -> 11008
 // 3320 / 3200, 172,800 x 5504 -> 2048 1545 / 1480, 8192 x 8192 -> 8192 413 / 400; the vendor's product with one scale
-// 3030, 1383, 341.
+// 3030, 1383, 341 (one board; this takes 3200 to 3360, 1480 to 1535, 400 from board to board).
 constexpr int kLargeSide = 256;
 constexpr int kLargeStage = 2 * kLargeSide * kStep;                  // bytes of a stage; XORed into LDS addresses
 constexpr int kLargeScales = 2 * kLargeStage, kLargeScaleBytes = 2 * kLargeSide * 4;
@@ -722,8 +722,11 @@ int launch_linear_large(LinearParams p, hipStream_t stream) {
 
 // Microseconds a shape takes: rounds of `slots` workgroups, each a fixed part and a part per step, a last round that
 // leaves slots empty less; at least what the bytes take.  Fitted to 3386 sizes of 65 ... 200,000 rows, 64 ... 5504
-// channels and 64 ... 11,008 features (mean deviation 4 to 6 %); what is taken by them is 0.3 % slower than the best
-// shape on average, more than 5 % at 55 sizes.
+// channels and 64 ... 11,008 features (mean deviation 4 to 6 %).  What is taken by all of choose_linear(), against the
+// best of the six forms (drawn sizes, channels and features as above): 6000 ... 200,000 rows 0.5 % slower on average, 8 %
+// or more at 2.1 % of 10,521 sizes, 31 % at worst (184,904 x 640 -> 256: 65 us, 256 x 256 tiles 50); 65 ... 6000 rows 0.3 %,
+// 8 % at 0.4 % of 28,427, 23 % at worst; 1 ... 64 rows 0.2 %, 8 % at 1.1 % of 18,201, 51 % at worst (35 x 2816 -> 4224: 14.2
+// us, shared 64 x 64 tiles 9.4).
 struct ShapeTime {
   double round, round_step;             // of a full round
   double last, last_step, last_filled;  // of the last: per step, and by how full it is
@@ -743,8 +746,7 @@ double shape_time(const ShapeTime& t, long long n_rows, int K, int F, int side, 
 }
 
 // The same of workgroups whose groups of waves share the channels, one per CU: for one round of tiles.  A part of the
-// steps is longer the more CUs work.  What is taken is 0.3 % slower than the best way on average over 10,000 sizes of up
-// to 6000 rows, 5504 channels and 11,008 features, more than 8 % at 1 % of them.
+// steps is longer the more CUs work.
 double shared_time(double fixed, double step, double step_filled, long long n_rows, int K, int F, int side, int groups) {
   const long long tiles = (n_rows + side - 1) / side * ((F + side - 1) / side);
   if (tiles > kCus) return 1e30;

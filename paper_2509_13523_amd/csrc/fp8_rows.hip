@@ -453,7 +453,7 @@ __device__ __forceinline__ float gate_far(float u, float v) {
   return __builtin_ldexpf(__builtin_ldexpf(v, half) * (factor * __builtin_amdgcn_exp2f((t - n) + rest)), e - half);
 }
 
-// Two blocks per group of lanes, read before either is worked on, and no more per workgroup: 172,800 rows x 5504 832 us,
+// Two blocks per group of lanes, read before either is worked on, and no more per workgroup: 172,800 rows x 5504 837 us,
 // 5.7 TB/s (one block at a time in 8192 workgroups 991; results that pass the caches like the rest 981).
 constexpr int kGateAhead = 2;
 __global__ __launch_bounds__(kThreads256) void swiglu_fp8_kernel(const bf16_t* __restrict__ uv, long long n_rows,
