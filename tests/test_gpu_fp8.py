@@ -969,3 +969,78 @@ def test_captured_products_and_gradients_of_many_tiles():
         torch.cuda.synchronize()
         assert all(same_bits(a, b) for a, b in zip(outs, want))
         torch.randn(1000, 1000, device="cuda").sum().item()
+
+
+# ------------------------------------------------------------------------------------- beyond 32 bits
+def around(border, n):
+    return np.unique(np.concatenate([[0, 1, 2 ** 31 // border, n - 257, n - 2, n - 1], np.arange(-2, 3) + 2 ** 32 // border]))
+
+
+def test_offsets_beyond_32_bits():
+    """Rows whose elements lie past 2^32 of each tensor: quantised, normalised, gated, multiplied, and their gradients."""
+    n, c, f = 2 ** 21 + 70001, 2048, 64
+    assert n * c > 2 ** 32 + 2 ** 27
+    gen = torch.Generator(device="cuda").manual_seed(73)
+    x = torch.empty(n, c, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    at = around(c, n)
+    xf = to_f64(x[at])
+    some = lambda q, scales, rows: codes(q[rows], scales.view(torch.uint8)[rows].view(torch.float8_e8m0fnu))
+
+    def same(got, want):
+        same_codes(got[0], want[0])
+        assert (got[1] == want[1]).all()
+    x8, xs, _, _ = B.aeris_fp8_quantize(x)
+    same(some(x8, xs, at), fo.quantize(xf))
+    # the norm without modulation
+    one, zero = torch.ones(c, device="cuda"), torch.zeros(1, c, device="cuda")
+    s, r, h8, hs = B.aeris_residual_norm_fp8_fwd(x, x, 1 + zero, one, zero, zero, 1e-6, n)
+    sf = to_f64(s[at])
+    assert (sf == 2 * xf).all()
+    h = sf / np.sqrt((sf ** 2).mean(1) + 1e-6)[:, None]
+    close_quantized("h", some(h8, hs, at), h, np.abs(h))
+    del s, h8, hs
+    # the gate of the rows as [u | v]
+    g8, gs = B.aeris_swiglu_fp8_fwd(x[:n // 2 * 2].view(n // 2, 2 * c))
+    half = around(2 * c, n // 2)
+    uv = to_f64(x[:n // 2 * 2].view(n // 2, 2 * c)[half])
+    g = bo.swiglu_fwd(uv)
+    close_quantized("g", some(g8, gs, half), g, np.abs(g))
+    del g8, gs
+    # products: a large operand, a large result; gradients with a large dx
+    w = torch.randn(f, c, device="cuda", generator=gen).bfloat16()
+    w8, ws, wt8, wts = B.aeris_fp8_quantize(w, transposed=True)
+    y = B.aeris_linear_fp8_fwd(x8, xs, w8, ws)
+    close_product("y", y[at], fo.dequantize(*some(x8, xs, at)), fo.dequantize(*codes(w8, ws)))
+    dx, dw = B.aeris_linear_fp8_bwd(x8, xs, wt8, wts, y)
+    close_product("dx", dx[at], fo.round_trip(to_f64(y[at])), fo.dequantize(*codes(wt8, wts)))
+    _, want = B.aeris_linear_bwd(drawn_values(x8, xs), w, y, want_dx=False)
+    assert torch.equal(dw, want)
+
+
+@pytest.mark.parametrize("c,f", [(2048, 320), (192, 2048)])
+def test_largest_tiles_beyond_32_bits(c, f):
+    """The 256 x 256 form on an operand and into a result of more than 2^32 elements."""
+    n = 2 ** 21 + 70001
+    assert n * max(c, f) > 2 ** 32 + 2 ** 27 and B.aeris_linear_fp8_plan(n, c, f)[0] == 256
+    gen = torch.Generator(device="cuda").manual_seed(c)
+    x8, xs, _, _ = B.aeris_fp8_quantize(torch.empty(n, c, dtype=torch.bfloat16, device="cuda").normal_(generator=gen))
+    w8, ws = drawn_operand(gen, f, c)
+    y = B.aeris_linear_fp8_fwd(x8, xs, w8, ws)
+    torch.cuda.synchronize()
+    at = around(max(c, f), n)
+    x = fo.dequantize(*codes(x8[at], xs.view(torch.uint8)[at].view(torch.float8_e8m0fnu)))
+    close_product("y", y[at], x, fo.dequantize(*codes(w8, ws)))
+
+
+def test_transpose_of_the_most_rows_and_columns():
+    """65,536 x 65,536: 2^32 elements, 512 blocks on either side."""
+    n = 65536
+    gen = torch.Generator(device="cuda").manual_seed(79)
+    x = torch.empty(n, n, dtype=torch.bfloat16, device="cuda").normal_(generator=gen)
+    x8, xs, xt8, xts = B.aeris_fp8_quantize(x, transposed=True)
+    torch.cuda.synchronize()
+    at = np.array([0, 1, 127, 128, 32767, 32768, 65407, 65408, 65534, 65535])
+    for (q, scales), part in (((x8, xs), x[at]), ((xt8, xts), x[:, at].t().contiguous())):
+        got, want = codes(q[at], scales.view(torch.uint8)[at].view(torch.float8_e8m0fnu)), fo.quantize(to_f64(part))
+        same_codes(got[0], want[0])
+        assert (got[1] == want[1]).all()
