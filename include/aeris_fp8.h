@@ -79,9 +79,9 @@ int aeris_residual_norm_fp8_fwd(const void* x, const void* y, const float* alpha
 
 /*
  * SwiGLU gate with its result quantised for the down-projection: g = silu(u) v, uv [n_rows, 2*hidden] =
- * [u | v] bf16; g8, gs = g quantised, without a rounding to bf16 before.  g is held wherever the format holds
- * it, also where silu(u) is below the normal numbers and v is large (aeris_swiglu_fwd gives zero from
- * u = -87.4 on).  An infinite u gives NaN.
+ * [u | v] bf16; g8, gs = g quantised, without a rounding to bf16 before.  g is held wherever fp32 and the
+ * format hold it, also where silu(u) is below the normal numbers and v is large (aeris_swiglu_fwd gives zero
+ * from u = -87.4 on).  An infinite u, or a g past fp32, gives NaN.
  * hidden % 64 == 0, hidden <= AERIS_MAX_FP8_COLUMNS.  Backward: aeris_swiglu_bwd.
  */
 int aeris_swiglu_fp8_fwd(const void* uv, int64_t n_rows, int32_t hidden, void* g8, void* gs,
