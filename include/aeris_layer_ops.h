@@ -101,7 +101,8 @@ int aeris_gate_residual_bwd(const void* y, const float* alpha, const void* dout,
 /*
  * SwiGLU gate (Model Architecture: SwiGLU in the fully connected layers) on the packed up
  * projection uv [n_rows, 2*hidden] = [u | v]:  g = silu(u) * v,  silu(u) = u / (1 + exp(-u)).
- * g is [n_rows, hidden] bf16.
+ * g is [n_rows, hidden] bf16.  From u = -87.4 on, where |silu(u)| < 1e-36, g is zero (also that of
+ * aeris_norm_linear_swiglu_fwd).
  */
 int aeris_swiglu_fwd(const void* uv, int64_t n_rows, int32_t hidden, void* g, void* hip_stream);
 
